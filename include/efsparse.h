@@ -61,8 +61,9 @@ extern "C" {
 #define EF_EINVAL 1     /* null / misaligned pointer, bad dtype or kind, density outside (0,1],
                            block < 1, segment table not a strictly increasing partition of [0,d),
                            layout not bound */
-#define EF_ERANGE 2     /* d == 0, d >= 2^31, n_seg < 1 or n_seg >= 2^24, W < 1 or W > 65535 */
-#define EF_EWORKSPACE 3 /* ws_bytes smaller than ef_workspace_bytes() */
+#define EF_ERANGE 2     /* d == 0, d >= 2^31, n_seg < 1 or n_seg >= 2^24, W < 1 or W > 65535; a
+                           linear layer's sizes outside their limits */
+#define EF_EWORKSPACE 3 /* ws_bytes smaller than ef_workspace_bytes() / ef_linear_workspace_bytes() */
 #define EF_EHIP 4       /* a HIP runtime or launch error */
 #define EF_ENOMEM 5     /* host memory for a layout's tables (or the timing records) could not be
                            allocated; a layout whose ef_layout_tune failed this way is unusable */
@@ -79,6 +80,22 @@ extern "C" {
 #define EF_OP_AGG_BLOCK 4
 #define EF_OP_AGG_SHARED 5
 #define EF_OP_RANDK_PREP 6
+
+/* workspace kinds for ef_linear_workspace_bytes */
+#define EF_OP_FORWARD 7
+#define EF_OP_DGRAD 8
+#define EF_OP_WGRAD 9
+
+/* formats of an 8-bit checkpoint */
+#define EF_CKPT_INT8 0  /* signed integers from -127 to 127 */
+#define EF_CKPT_E4M3 1  /* 4 bits of exponent, 3 of mantissa (the OCP type without infinities) */
+
+/* activations */
+#define EF_ACT_NONE 0
+#define EF_ACT_RELU 1       /* max(z, 0) */
+#define EF_ACT_GELU 2       /* z Phi(z), Phi the normal distribution function */
+#define EF_ACT_GELU_TANH 3  /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+#define EF_ACT_SILU 4       /* z / (1 + exp(-z)) */
 
 /* message kinds */
 #define EF_MSG_SPARSE 0
@@ -370,6 +387,92 @@ int ef_step_randk_prepared_batch(const ef_layout* layout, int32_t W, const void*
  * range regardless).  The word is only ever OR-ed: clear it to watch a given
  * call.  Returns (size_t)-1 for other ops. */
 size_t ef_workspace_diag_offset(const ef_layout* layout, int op);
+
+/* The checkpointed linear layer: where a worker's gradient comes from.
+ *
+ * Between the forward and the backward pass a layer's activations are kept
+ * in 8 bits, a checkpoint; the backward products read it as it is, and the
+ * weight gradient is written into the flat gradient g, or added to the
+ * error-feedback memory e (Algorithm 1's acc = g + e without g in between:
+ * bitwise ef_accumulate of the written gradient).
+ *
+ * Checkpoint of a matrix [n][c]: with G = ceil(c / 32),
+ *   codes   uint8[n][32 G] (ef_ckpt_row_bytes(c) a row), 16-byte aligned
+ *   scales  uint8[n][G]
+ * Columns [32 g, 32 g + 32) of a row are a group with one power of two 2^e,
+ * scales = e + 127: the smallest e >= -100 under which the group's largest
+ * magnitude rounds to 127 or less (EF_CKPT_INT8) or is at most 448 * 2^e
+ * (EF_CKPT_E4M3).  codes = value / 2^e rounded to nearest, ties to even;
+ * the columns past c hold code 0.  A group with an infinity or a NaN has
+ * scale 255 and codes 0 and stands for NaN, so an overflow stays visible in
+ * every gradient that it reaches.  Decoded values code * 2^e are exact in
+ * bfloat16.  Rows stand by themselves: rows [a, b) of a checkpoint are the
+ * checkpoint of those rows.
+ *
+ * Shared by these calls:
+ *  - n tokens (rows; 0 is allowed and does nothing, or gives a gradient of
+ *    zeros), i input and o output features; 0 <= n < 2^31, 1 <= i, c, o
+ *    <= 2^26, else EF_ERANGE.
+ *  - Matrices are row-major with a leading dimension ld (elements between
+ *    rows) of at least their columns; any element-aligned address and any ld
+ *    is taken (rows that start on 16 bytes are read fastest).  dtype is
+ *    EF_F32 or EF_BF16, one for all matrices of a call.
+ *  - Products and sums are held in float32 and rounded once, where they are
+ *    stored.  The order of every sum is fixed by the sizes: results are
+ *    bitwise reproducible.
+ *  - Outputs must not overlap inputs, except where a call says so
+ *    (EF_EINVAL).
+ *  - ws: 256-byte aligned, at least ef_linear_workspace_bytes bytes (may be
+ *    null where that is 0); contents need not be preserved. */
+int64_t ef_ckpt_row_bytes(int64_t c);
+
+/* codes, scales = the checkpoint of x [n][c]. */
+int ef_ckpt_pack(int64_t n, int64_t c, const void* x, int64_t ldx, int dtype, int fmt, uint8_t* codes,
+                 uint8_t* scales, void* stream);
+
+/* y [n][c] = what the checkpoint stands for. */
+int ef_ckpt_unpack(int64_t n, int64_t c, const uint8_t* codes, const uint8_t* scales, int fmt, void* y,
+                   int64_t ldy, int dtype, void* stream);
+
+/* Backward through an activation whose input z was kept: dz = dy * act'(z),
+ * [n][c].  dz may be dy itself (same ld). */
+int ef_ckpt_act_backward(int64_t n, int64_t c, int act, const uint8_t* codes, const uint8_t* scales, int fmt,
+                         const void* dy, int64_t lddy, void* dz, int64_t lddz, int dtype, void* stream);
+
+/* Workspace of a product (op EF_OP_FORWARD, EF_OP_DGRAD or EF_OP_WGRAD; dtype
+ * that of its matrices).  0 where none is needed, and for arguments that the
+ * call would refuse. */
+size_t ef_linear_workspace_bytes(int op, int64_t n, int64_t i, int64_t o, int dtype);
+
+/* The layer's forward pass, for any number of tokens from one:
+ *   z = x w^T + bias    x [n][i], w [o][i], bias [o] or null
+ *   codes, scales = the checkpoint of z (where not null; both or neither)
+ *   y = act(z) + res    res [n][o] or null, may be y itself (same ld)
+ * z itself is never stored. */
+int ef_linear_forward(int64_t n, int64_t i, int64_t o, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                      const void* bias, int act, const void* res, int64_t ldr, void* y, int64_t ldy, int dtype,
+                      uint8_t* codes, uint8_t* scales, int fmt, void* ws, size_t ws_bytes, void* stream);
+
+/* The gradient of the layer's input, and on through the activation that made
+ * that input:
+ *   dx = (dy w) * act'(z) + res     dy [n][o], w [o][i], dx [n][i]
+ * z [n][i] the kept input of that activation (codes and scales are not read
+ * with EF_ACT_NONE), res [n][i] or null the gradient that reached it another
+ * way (a skip connection); res may be dx itself (same ld). */
+int ef_linear_dgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t lddy, const void* w, int64_t ldw,
+                    int act, const uint8_t* codes, const uint8_t* scales, int fmt, const void* res, int64_t ldr,
+                    void* dx, int64_t lddx, int dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* The gradient of the layer's weights and bias, from the kept input x [n][i]:
+ *   dw = dy^T x     [o][i], contiguous (a segment of the flat gradient)
+ *   db = the sum of dy's rows, [o], or null
+ * of type g_dtype, rounded once; with accumulate (EF_F32 only) dw += and
+ * db += instead: each fl32(old + sum), the error-feedback memory's
+ * accumulate step.  The rows of padded tokens take part: they add nothing
+ * where dy holds zeros and the kept row is finite. */
+int ef_linear_wgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t lddy, int dtype,
+                    const uint8_t* codes, const uint8_t* scales, int fmt, void* dw, void* db, int g_dtype,
+                    int accumulate, void* ws, size_t ws_bytes, void* stream);
 
 /* Per-kernel timing (diagnostics).  While enabled, every kernel the library
  * launches carries a start and a stop HIP event that the runtime binds to the

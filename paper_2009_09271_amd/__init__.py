@@ -22,6 +22,9 @@ LIB_PATH = os.environ.get("EFSPARSE_LIB") or os.path.join(_HERE, "libefsparse.so
 EF_OK, EF_EINVAL, EF_ERANGE, EF_EWORKSPACE, EF_EHIP, EF_ENOMEM = range(6)
 EF_F32, EF_BF16 = 0, 1
 EF_OP_TOPK, EF_OP_RANDK, EF_OP_RANDBLOCK, EF_OP_AGG_SPARSE, EF_OP_AGG_BLOCK, EF_OP_AGG_SHARED, EF_OP_RANDK_PREP = range(7)
+EF_OP_FORWARD, EF_OP_DGRAD, EF_OP_WGRAD = 7, 8, 9
+EF_CKPT_INT8, EF_CKPT_E4M3 = 0, 1
+EF_ACT_NONE, EF_ACT_RELU, EF_ACT_GELU, EF_ACT_GELU_TANH, EF_ACT_SILU = range(5)
 EF_MSG_SPARSE, EF_MSG_BLOCK = 0, 1
 EF_TUNE_RANDK_SIGMA, EF_TUNE_RANDK_EXTRA, EF_TUNE_TOPK_SIGMA, EF_TUNE_TOPK_EXTRA, EF_TUNE_TOPK_RETRY, EF_TUNE_POOL = range(6)
 EF_PHASE_PREPARE, EF_PHASE_STREAM, EF_PHASE_FINISH, EF_PHASE_ALL = 1, 2, 4, 7
@@ -84,6 +87,19 @@ _SIGS = {
     "ef_step_topk_phases": (_c.c_int, [_P, _c.c_uint, _P, _c.c_int, _P, _P, _P, _P, _c.c_size_t, _P]),
     "ef_step_randk_phases": (_c.c_int, [_P, _c.c_uint, _P, _c.c_int, _P, _c.c_uint64, _c.c_uint32, _P, _P, _P,
                                         _c.c_size_t, _P]),
+    "ef_ckpt_row_bytes": (_c.c_int64, [_c.c_int64]),
+    "ef_ckpt_pack": (_c.c_int, [_c.c_int64, _c.c_int64, _P, _c.c_int64, _c.c_int, _c.c_int, _P, _P, _P]),
+    "ef_ckpt_unpack": (_c.c_int, [_c.c_int64, _c.c_int64, _P, _P, _c.c_int, _P, _c.c_int64, _c.c_int, _P]),
+    "ef_ckpt_act_backward": (_c.c_int, [_c.c_int64, _c.c_int64, _c.c_int, _P, _P, _c.c_int, _P, _c.c_int64, _P,
+                                        _c.c_int64, _c.c_int, _P]),
+    "ef_linear_workspace_bytes": (_c.c_size_t, [_c.c_int, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int]),
+    "ef_linear_forward": (_c.c_int, [_c.c_int64, _c.c_int64, _c.c_int64, _P, _c.c_int64, _P, _c.c_int64, _P, _c.c_int,
+                                     _P, _c.c_int64, _P, _c.c_int64, _c.c_int, _P, _P, _c.c_int, _P, _c.c_size_t,
+                                     _P]),
+    "ef_linear_dgrad": (_c.c_int, [_c.c_int64, _c.c_int64, _c.c_int64, _P, _c.c_int64, _P, _c.c_int64, _c.c_int, _P,
+                                   _P, _c.c_int, _P, _c.c_int64, _P, _c.c_int64, _c.c_int, _P, _c.c_size_t, _P]),
+    "ef_linear_wgrad": (_c.c_int, [_c.c_int64, _c.c_int64, _c.c_int64, _P, _c.c_int64, _c.c_int, _P, _P, _c.c_int,
+                                   _P, _P, _c.c_int, _c.c_int, _P, _c.c_size_t, _P]),
     "ef_timing_enable": (_c.c_int, [_c.c_int]),
     "ef_timing_collect": (_c.c_int, []),
     "ef_timing_count": (_c.c_int, []),
@@ -483,6 +499,180 @@ def ef_step_randblock(layout, g, e, seed, step, start, val, stream=None):
     _step_args(layout, g, e, start, val, False, w, idx_len=layout.n_seg)
     _check(_lib.ef_step_randblock(layout.handle, _ptr(g), _gdt(g), _ptr(e), int(seed), int(step), _ptr(start),
                                   _ptr(val), _stream(e, stream)), w)
+
+
+# ---- the checkpointed linear layer ----
+# Matrices are two-dimensional tensors whose rows are contiguous (any row stride of at least a row); all of a call's
+# tensors are on one GPU, whose current stream (or `stream`) the call is enqueued on.
+
+def _arg(t, name, where, dtypes, rows=None, cols=None, dev=None):
+    """Checks a matrix argument (a vector where rows is 0) before its pointer crosses the ABI."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise EfError(EF_EINVAL, where, f"{name} is None" if t is None else f"{name} is not a tensor")
+    if not t.is_cuda:
+        raise EfError(EF_EINVAL, where, f"{name} is not on a GPU")
+    if dev is not None and t.device != dev:
+        raise EfError(EF_EINVAL, where, f"{name} is on {t.device}, not on {dev}")
+    if t.dtype not in dtypes:
+        raise EfError(EF_EINVAL, where, f"{name} has dtype {t.dtype}")
+    if rows == 0:
+        if t.dim() != 1 or t.shape[0] != cols or (cols > 1 and t.stride(0) != 1):
+            raise EfError(EF_EINVAL, where, f"{name} is not a contiguous vector of {cols}")
+        return t
+    if t.dim() != 2:
+        raise EfError(EF_EINVAL, where, f"{name} is not a matrix")
+    n, c = t.shape
+    if (rows is not None and n != rows[0]) or (cols is not None and c != cols):
+        raise EfError(EF_EINVAL, where, f"{name} has shape {tuple(t.shape)}, "
+                                        f"{(rows[0] if rows is not None else n, cols if cols is not None else c)} needed")
+    if c > 1 and t.stride(1) != 1 or n > 1 and t.stride(0) < c:
+        raise EfError(EF_EINVAL, where, f"{name} has strides {tuple(t.stride())}: its rows must be contiguous and apart")
+    return t
+
+
+def _ld(t):
+    """Elements from one row to the next (a single row's own length, whatever its stride says)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _kept(codes, scales, n, c, where, dev):
+    import torch
+    g = (c + 31) // 32
+    for t, name, w in ((codes, "codes", 32 * g), (scales, "scales", g)):
+        _arg(t, name, where, (torch.uint8,), (n,), w, dev)
+        if n > 1 and t.stride(0) != w:
+            raise EfError(EF_EINVAL, where, f"{name} is not contiguous")
+
+
+def _mats():
+    import torch
+    return (torch.float32, torch.bfloat16)
+
+
+def _enqueue(fn, where, t, stream, *args):
+    """Calls the library with t's device current, on `stream` or that device's current stream."""
+    import torch
+    if t.device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream(t, stream)), where)
+    else:
+        with torch.cuda.device(t.device):
+            _check(fn(*args, _stream(t, stream)), where)
+
+
+def ckpt_buffers(n, c, device="cuda"):
+    """(codes, scales) for the checkpoint of an [n][c] matrix."""
+    import torch
+    return (torch.empty((n, (c + 31) // 32 * 32), dtype=torch.uint8, device=device),
+            torch.empty((n, (c + 31) // 32), dtype=torch.uint8, device=device))
+
+
+def linear_workspace(op, n, i, o, dtype, device="cuda"):
+    """A workspace for EF_OP_FORWARD, EF_OP_DGRAD or EF_OP_WGRAD of these sizes (dtype: torch.float32 or
+    torch.bfloat16); products of several sizes may share the largest."""
+    import torch
+    code = {torch.float32: EF_F32, torch.bfloat16: EF_BF16}.get(dtype)
+    if code is None:
+        raise TypeError(f"dtype {dtype} not supported (float32 or bfloat16)")
+    n = int(_lib.ef_linear_workspace_bytes(int(op), int(n), int(i), int(o), code))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def _ws(ws, where, dev):
+    if ws is not None and (not ws.is_cuda or ws.device != dev or not ws.is_contiguous()):
+        raise EfError(EF_EINVAL, where, f"ws is not a contiguous tensor on {dev}")
+    return _ptr(ws), _nbytes(ws)
+
+
+def ef_ckpt_pack(x, codes, scales, fmt=EF_CKPT_INT8, stream=None):
+    """codes, scales = the 8-bit checkpoint of x [n][c]."""
+    w = "ef_ckpt_pack"
+    _arg(x, "x", w, _mats())
+    n, c = x.shape
+    _kept(codes, scales, n, c, w, x.device)
+    _enqueue(_lib.ef_ckpt_pack, w, x, stream, n, c, _ptr(x), _ld(x), _gdt(x), int(fmt), _ptr(codes), _ptr(scales))
+
+
+def ef_ckpt_unpack(codes, scales, fmt, y, stream=None):
+    """y [n][c] = what a checkpoint stands for."""
+    w = "ef_ckpt_unpack"
+    _arg(y, "y", w, _mats())
+    n, c = y.shape
+    _kept(codes, scales, n, c, w, y.device)
+    _enqueue(_lib.ef_ckpt_unpack, w, y, stream, n, c, _ptr(codes), _ptr(scales), int(fmt), _ptr(y), _ld(y), _gdt(y))
+
+
+def ef_ckpt_act_backward(act, codes, scales, fmt, dy, dz, stream=None):
+    """dz = dy * act'(z), z the kept input of the activation; dz may be dy."""
+    w = "ef_ckpt_act_backward"
+    _arg(dy, "dy", w, _mats())
+    n, c = dy.shape
+    _arg(dz, "dz", w, (dy.dtype,), (n,), c, dy.device)
+    _kept(codes, scales, n, c, w, dy.device)
+    _enqueue(_lib.ef_ckpt_act_backward, w, dy, stream, n, c, int(act), _ptr(codes), _ptr(scales), int(fmt), _ptr(dy),
+             _ld(dy), _ptr(dz), _ld(dz), _gdt(dy))
+
+
+def ef_linear_forward(x, weight, y, ws, bias=None, act=EF_ACT_NONE, res=None, codes=None, scales=None,
+                      fmt=EF_CKPT_INT8, stream=None):
+    """y = act(z) + res, z = x weight^T + bias; codes, scales (both or neither) receive the checkpoint of z.
+    x [n][i], weight [o][i], y and res [n][o], bias [o]; res may be y."""
+    w = "ef_linear_forward"
+    _arg(x, "x", w, _mats())
+    dev, t = x.device, (x.dtype,)
+    n, i = x.shape
+    _arg(weight, "weight", w, t, None, i, dev)
+    o = weight.shape[0]
+    _arg(y, "y", w, t, (n,), o, dev)
+    if bias is not None:
+        _arg(bias, "bias", w, t, 0, o, dev)
+    if res is not None:
+        _arg(res, "res", w, t, (n,), o, dev)
+    if codes is not None or scales is not None:
+        _kept(codes, scales, n, o, w, dev)
+    _enqueue(_lib.ef_linear_forward, w, x, stream, n, i, o, _ptr(x), _ld(x), _ptr(weight), _ld(weight), _ptr(bias),
+             int(act), _ptr(res), _ld(res) if res is not None else 0, _ptr(y), _ld(y), _gdt(x), _ptr(codes),
+             _ptr(scales), int(fmt), *_ws(ws, w, dev))
+
+
+def ef_linear_dgrad(dy, weight, dx, ws, act=EF_ACT_NONE, codes=None, scales=None, fmt=EF_CKPT_INT8, res=None,
+                    stream=None):
+    """dx = (dy weight) * act'(z) + res, z the kept input of the activation before the layer.
+    dy [n][o], weight [o][i], dx and res [n][i]; res may be dx."""
+    w = "ef_linear_dgrad"
+    _arg(dy, "dy", w, _mats())
+    dev, t = dy.device, (dy.dtype,)
+    n, o = dy.shape
+    _arg(weight, "weight", w, t, (o,), None, dev)
+    i = weight.shape[1]
+    _arg(dx, "dx", w, t, (n,), i, dev)
+    if res is not None:
+        _arg(res, "res", w, t, (n,), i, dev)
+    if act != EF_ACT_NONE:
+        _kept(codes, scales, n, i, w, dev)
+    else:
+        codes = scales = None
+    _enqueue(_lib.ef_linear_dgrad, w, dy, stream, n, i, o, _ptr(dy), _ld(dy), _ptr(weight), _ld(weight), int(act),
+             _ptr(codes), _ptr(scales), int(fmt), _ptr(res), _ld(res) if res is not None else 0, _ptr(dx), _ld(dx),
+             _gdt(dy), *_ws(ws, w, dev))
+
+
+def ef_linear_wgrad(dy, codes, scales, fmt, dw, ws, db=None, accumulate=False, stream=None):
+    """dw = dy^T x, db = the sum of dy's rows (accumulate: added to what they hold), x the kept input of the layer.
+    dy [n][o], dw [o][i] contiguous (a segment of the flat gradient or of the error-feedback memory), db [o]."""
+    w = "ef_linear_wgrad"
+    _arg(dy, "dy", w, _mats())
+    dev = dy.device
+    n, o = dy.shape
+    _arg(dw, "dw", w, _mats(), (o,), None, dev)
+    i = dw.shape[1]
+    if o > 1 and dw.stride(0) != i:
+        raise EfError(EF_EINVAL, w, "dw is not contiguous")
+    if db is not None:
+        _arg(db, "db", w, (dw.dtype,), 0, o, dev)
+    _kept(codes, scales, n, i, w, dev)
+    _enqueue(_lib.ef_linear_wgrad, w, dy, stream, n, i, o, _ptr(dy), _ld(dy), _gdt(dy), _ptr(codes), _ptr(scales),
+             int(fmt), _ptr(dw), _ptr(db), _gdt(dw), 1 if accumulate else 0, *_ws(ws, w, dev))
 
 
 def lib():

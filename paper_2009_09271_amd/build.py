@@ -7,9 +7,10 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(HERE, "csrc", "efsparse.hip")
+SRCS = [os.path.join(HERE, "csrc", f) for f in ("efsparse.hip", "linear.hip")]
 OUT = os.path.join(HERE, "libefsparse.so")
 
 FLAGS = [
@@ -17,7 +18,6 @@ FLAGS = [
     "-O3",
     "-std=c++17",
     "-fPIC",
-    "-shared",
     "-ffp-contract=off",            # no fused multiply-add contraction: IEEE add / divide only
     "-Wall",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -33,10 +33,20 @@ def hipcc():
 
 def build(verbose: bool = False) -> str:
     tmp = OUT + ".tmp"
-    cmd = [hipcc()] + FLAGS + [SRC, "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
+    with tempfile.TemporaryDirectory() as d:
+        jobs = []
+        for src in SRCS:  # side by side
+            cmd = [hipcc()] + FLAGS + ["-c", src, "-o", os.path.join(d, os.path.basename(src) + ".o")]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            jobs.append((cmd, subprocess.Popen(cmd)))
+        failed = [cmd for cmd, p in jobs if p.wait()]
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC"] + [cmd[-1] for cmd, _ in jobs] + ["-o", tmp]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.check_call(cmd)
     os.replace(tmp, OUT)
     return OUT
 

@@ -1,9 +1,6 @@
 // efsparse host library: layouts, argument checking, workspace layout and kernel launches.
 // The C ABI is declared in include/efsparse.h.
 
-#include <hip/hip_ext.h>
-#include <hip/hip_runtime.h>
-
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -14,7 +11,7 @@
 #include <string>
 #include <vector>
 
-#include "../../include/efsparse.h"
+#include "ef_host.h"
 #include "ef_kernels.h"
 
 using namespace efs;
@@ -28,11 +25,7 @@ static __device__ __align__(256) uint8_t scratch[kNoAllocScratch];
 
 namespace {
 
-constexpr size_t kAlign = 256;
-
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 int32_t agg_tiles(int64_t d) { return (int32_t)((d + kAggTile - 1) / kAggTile); }
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 // Packs int32 / uint64 host arrays into one blob with 256-byte aligned sub-arrays.
 struct Blob {
@@ -467,17 +460,7 @@ WSel make_ws(const WsLayout& l, void* base) {
   return w;
 }
 
-hipStream_t S(void* s) { return reinterpret_cast<hipStream_t>(s); }
-
 thread_local int g_last_hip_error = 0;
-
-int hip_status(hipError_t e) {
-  if (e == hipSuccess) return EF_OK;
-  g_last_hip_error = (int)e;
-  return EF_EHIP;
-}
-
-int launched() { return hip_status(hipGetLastError()); }
 
 // ---- optional per-kernel timing: HIP events recorded around each launch on its stream ----
 struct TimingRec {
@@ -506,9 +489,15 @@ hipEvent_t pool_event() {
   return e;
 }
 
-// While timing is on, a launch gets a start and a stop event that the runtime ties to the kernel's
-// own dispatch (hipExtLaunchKernelGGL), so the elapsed time is the kernel's execution alone.
-bool timing_slot(const char* name, hipEvent_t* a, hipEvent_t* b) {
+}  // namespace
+
+int efs::hip_status(hipError_t e) {
+  if (e == hipSuccess) return EF_OK;
+  g_last_hip_error = (int)e;
+  return EF_EHIP;
+}
+
+bool efs::timing_slot(const char* name, hipEvent_t* a, hipEvent_t* b) {
   if (!g_timing.load(std::memory_order_relaxed)) return false;
   std::lock_guard<std::mutex> lk(g_tm);
   TimingRec r{name, pool_event(), pool_event()};
@@ -525,21 +514,7 @@ bool timing_slot(const char* name, hipEvent_t* a, hipEvent_t* b) {
   return true;
 }
 
-// Every launch goes through this macro: the kernel is named after its expression.
-#define EF_LAUNCH(KERNEL, GRID, BLOCK, SHM, ST, ...)                                   \
-  do {                                                                                 \
-    hipEvent_t _ea = nullptr, _eb = nullptr;                                           \
-    if (timing_slot(#KERNEL, &_ea, &_eb))                                              \
-      hipExtLaunchKernelGGL(KERNEL, GRID, BLOCK, SHM, ST, _ea, _eb, 0u, __VA_ARGS__); \
-    else                                                                               \
-      hipLaunchKernelGGL(KERNEL, GRID, BLOCK, SHM, ST, __VA_ARGS__);                  \
-  } while (0)
-
-#define EF_TRY(x)              \
-  do {                         \
-    const int _rc = (x);       \
-    if (_rc != EF_OK) return _rc; \
-  } while (0)
+namespace {
 
 int check_bound(const ef_layout* L) {
   if (!L || !L->valid || !L->bound) return EF_EINVAL;

@@ -1,0 +1,225 @@
+// Host side of the checkpointed linear layer: argument checking, workspaces and launches.
+// The C ABI is declared in include/efsparse.h, the kernels are in ef_linear.h.
+
+#include "ef_host.h"
+#include "ef_linear.h"
+
+#include <algorithm>
+
+using namespace efs;
+
+namespace {
+
+constexpr int64_t kMaxWidth = (int64_t)1 << 26;  // columns, and output features
+constexpr int64_t kMaxRows = (int64_t)1 << 31;
+constexpr int64_t kMaxGrid = 0x7FFFFFFF;
+
+bool dtype_ok(int t) { return t == EF_F32 || t == EF_BF16; }
+bool fmt_ok(int f) { return f == EF_CKPT_INT8 || f == EF_CKPT_E4M3; }
+bool act_ok(int a) { return a >= EF_ACT_NONE && a <= EF_ACT_SILU; }
+int64_t bytes_of(int t) { return t == EF_F32 ? 4 : 2; }
+int32_t groups(int64_t c) { return (int32_t)((c + kGroup - 1) / kGroup); }
+
+// A matrix argument: aligned to its elements, rows at least as far apart as they are long.
+bool mat_ok(const void* p, int64_t rows, int64_t cols, int64_t ld, int t) {
+  return ld >= cols && ld < ((int64_t)1 << 40) && (rows == 0 || (p && aligned(p, (size_t)bytes_of(t))));
+}
+
+bool kept_ok(const uint8_t* codes, const uint8_t* scales, int64_t rows) {
+  return rows == 0 || (codes && scales && aligned(codes, 16));
+}
+
+struct Range {
+  const char *a, *b;
+};
+Range range(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t size) {
+  const char* q = static_cast<const char*>(p);
+  if (!q || !rows) return {nullptr, nullptr};
+  return {q, q + ((rows - 1) * ld + cols) * size};
+}
+Range range_kept(const uint8_t* codes, int64_t rows, int64_t c) {
+  const int64_t row = (int64_t)groups(c) * kGroup;
+  return range(codes, rows, row, row, 1);
+}
+Range range_scales(const uint8_t* s, int64_t rows, int64_t c) { return range(s, rows, groups(c), groups(c), 1); }
+bool meet(Range x, Range y) { return x.a < y.b && y.a < x.b; }
+template <typename... R> bool meet_any(Range x, R... y) { return (meet(x, y) || ...); }
+
+// Grid of the elementwise passes: lanes per row (as a power of two's exponent), rows and columns of workgroups.
+struct Flat {
+  dim3 grid;
+  int txs;
+};
+int flat_of(int64_t n, int64_t c, Flat* f) {
+  const int64_t lanes = (int64_t)groups(c) * 4;
+  int txs = 2;
+  while (txs < 8 && ((int64_t)1 << txs) < lanes) ++txs;
+  const int64_t gx = (n + (256 >> txs) - 1) / (256 >> txs), gy = (lanes + ((int64_t)1 << txs) - 1) >> txs;
+  if (gx > kMaxGrid || gy > 65535) return EF_ERANGE;
+  f->grid = dim3((unsigned)gx, (unsigned)gy);
+  f->txs = txs;
+  return EF_OK;
+}
+
+// One product: sizes of C and of the sum, the operands and the epilogue.
+struct Product {
+  int64_t M, N, K;
+  Mat A, B;
+  Kept BK;
+  Epi ep;
+};
+
+int check_sizes(int64_t n, int64_t i, int64_t o) {
+  if (n < 0 || n >= kMaxRows || i < 1 || i > kMaxWidth || o < 1 || o > kMaxWidth) return EF_ERANGE;
+  return EF_OK;
+}
+
+template <int KIND, int DT, int DO>
+int run_product(const Product& p, hipStream_t st) {
+  const int64_t tiles = ((p.M + kAnyTile - 1) / kAnyTile) * ((p.N + kAnyTile - 1) / kAnyTile);
+  if (tiles > kMaxGrid) return EF_ERANGE;
+  EF_LAUNCH((k_linear_any<KIND, DT, DO>), dim3((unsigned)tiles), dim3(256), 0, st, (int32_t)p.M, (int32_t)p.N,
+            (int32_t)p.K, p.A, p.B, p.BK, p.ep);
+  return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t ef_ckpt_row_bytes(int64_t c) { return c < 1 || c > kMaxWidth ? 0 : (int64_t)groups(c) * kGroup; }
+
+int ef_ckpt_pack(int64_t n, int64_t c, const void* x, int64_t ldx, int dtype, int fmt, uint8_t* codes,
+                 uint8_t* scales, void* stream) {
+  EF_TRY(check_sizes(n, c, 1));
+  if (!dtype_ok(dtype) || !fmt_ok(fmt) || !mat_ok(x, n, c, ldx, dtype) || !kept_ok(codes, scales, n)) return EF_EINVAL;
+  const Range q = range_kept(codes, n, c), s = range_scales(scales, n, c);
+  if (meet(q, s) || meet_any(range(x, n, c, ldx, bytes_of(dtype)), q, s)) return EF_EINVAL;
+  if (n == 0) return EF_OK;
+  Flat f;
+  EF_TRY(flat_of(n, c, &f));
+  const Kept k{codes, scales, groups(c), fmt};
+  if (dtype == EF_F32) EF_LAUNCH(k_ckpt_pack<EF_F32>, f.grid, dim3(256), 0, S(stream), n, (int32_t)c, x, ldx, k, f.txs);
+  else EF_LAUNCH(k_ckpt_pack<EF_BF16>, f.grid, dim3(256), 0, S(stream), n, (int32_t)c, x, ldx, k, f.txs);
+  return launched();
+}
+
+int ef_ckpt_unpack(int64_t n, int64_t c, const uint8_t* codes, const uint8_t* scales, int fmt, void* y, int64_t ldy,
+                   int dtype, void* stream) {
+  EF_TRY(check_sizes(n, c, 1));
+  if (!dtype_ok(dtype) || !fmt_ok(fmt) || !mat_ok(y, n, c, ldy, dtype) || !kept_ok(codes, scales, n)) return EF_EINVAL;
+  if (meet_any(range(y, n, c, ldy, bytes_of(dtype)), range_kept(codes, n, c), range_scales(scales, n, c)))
+    return EF_EINVAL;
+  if (n == 0) return EF_OK;
+  Flat f;
+  EF_TRY(flat_of(n, c, &f));
+  const Kept k{const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), groups(c), fmt};
+  if (dtype == EF_F32) EF_LAUNCH(k_ckpt_unpack<EF_F32>, f.grid, dim3(256), 0, S(stream), n, (int32_t)c, k, y, ldy, f.txs);
+  else EF_LAUNCH(k_ckpt_unpack<EF_BF16>, f.grid, dim3(256), 0, S(stream), n, (int32_t)c, k, y, ldy, f.txs);
+  return launched();
+}
+
+int ef_ckpt_act_backward(int64_t n, int64_t c, int act, const uint8_t* codes, const uint8_t* scales, int fmt,
+                         const void* dy, int64_t lddy, void* dz, int64_t lddz, int dtype, void* stream) {
+  EF_TRY(check_sizes(n, c, 1));
+  if (!dtype_ok(dtype) || !fmt_ok(fmt) || !act_ok(act) || !mat_ok(dy, n, c, lddy, dtype) ||
+      !mat_ok(dz, n, c, lddz, dtype) || !kept_ok(codes, scales, n))
+    return EF_EINVAL;
+  const Range out = range(dz, n, c, lddz, bytes_of(dtype));
+  if (meet_any(out, range_kept(codes, n, c), range_scales(scales, n, c))) return EF_EINVAL;
+  if (meet(out, range(dy, n, c, lddy, bytes_of(dtype))) && !(dz == dy && lddz == lddy)) return EF_EINVAL;
+  if (n == 0) return EF_OK;
+  Flat f;
+  EF_TRY(flat_of(n, c, &f));
+  const Kept k{const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), groups(c), fmt};
+  if (dtype == EF_F32)
+    EF_LAUNCH(k_ckpt_act_backward<EF_F32>, f.grid, dim3(256), 0, S(stream), n, (int32_t)c, act, k, dy, lddy, dz, lddz, f.txs);
+  else
+    EF_LAUNCH(k_ckpt_act_backward<EF_BF16>, f.grid, dim3(256), 0, S(stream), n, (int32_t)c, act, k, dy, lddy, dz, lddz, f.txs);
+  return launched();
+}
+
+size_t ef_linear_workspace_bytes(int op, int64_t n, int64_t i, int64_t o, int dtype) {
+  if (check_sizes(n, i, o) != EF_OK || !dtype_ok(dtype) || op < EF_OP_FORWARD || op > EF_OP_WGRAD) return 0;
+  return 0;
+}
+
+int ef_linear_forward(int64_t n, int64_t i, int64_t o, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                      const void* bias, int act, const void* res, int64_t ldr, void* y, int64_t ldy, int dtype,
+                      uint8_t* codes, uint8_t* scales, int fmt, void* ws, size_t ws_bytes, void* stream) {
+  EF_TRY(check_sizes(n, i, o));
+  if (!dtype_ok(dtype) || !act_ok(act) || !mat_ok(x, n, i, ldx, dtype) || !mat_ok(w, o, i, ldw, dtype) ||
+      !mat_ok(y, n, o, ldy, dtype) || (bias && !aligned(bias, (size_t)bytes_of(dtype))) ||
+      (res && !mat_ok(res, n, o, ldr, dtype)) || !codes != !scales)
+    return EF_EINVAL;
+  if (codes && (!fmt_ok(fmt) || !kept_ok(codes, scales, n))) return EF_EINVAL;
+  const int64_t b = bytes_of(dtype);
+  const Range out = range(y, n, o, ldy, b), rx = range(x, n, i, ldx, b), rw = range(w, o, i, ldw, b),
+              rb = range(bias, 1, o, o, b), rr = range(res, n, o, ldr, b),
+              q = codes ? range_kept(codes, n, o) : Range{nullptr, nullptr},
+              s = codes ? range_scales(scales, n, o) : Range{nullptr, nullptr};
+  if (meet_any(out, rx, rw, rb, q, s) || meet_any(q, s, rx, rw, rb, rr) || meet_any(s, rx, rw, rb, rr)) return EF_EINVAL;
+  if (meet(out, rr) && !(res == y && ldr == ldy)) return EF_EINVAL;
+  if (n == 0) return EF_OK;
+  Product p{n, o, i, {x, ldx}, {w, ldw}, {}, {y, ldy, bias, res, ldr, {codes, scales, groups(o), fmt}, act, 0}};
+  return dtype == EF_F32 ? run_product<K_FWD, EF_F32, EF_F32>(p, S(stream))
+                         : run_product<K_FWD, EF_BF16, EF_BF16>(p, S(stream));
+}
+
+int ef_linear_dgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t lddy, const void* w, int64_t ldw, int act,
+                    const uint8_t* codes, const uint8_t* scales, int fmt, const void* res, int64_t ldr, void* dx,
+                    int64_t lddx, int dtype, void* ws, size_t ws_bytes, void* stream) {
+  EF_TRY(check_sizes(n, i, o));
+  if (!dtype_ok(dtype) || !act_ok(act) || !mat_ok(dy, n, o, lddy, dtype) || !mat_ok(w, o, i, ldw, dtype) ||
+      !mat_ok(dx, n, i, lddx, dtype) || (res && !mat_ok(res, n, i, ldr, dtype)))
+    return EF_EINVAL;
+  const bool kept = act != EF_ACT_NONE;
+  if (kept && (!fmt_ok(fmt) || !kept_ok(codes, scales, n))) return EF_EINVAL;
+  const int64_t b = bytes_of(dtype);
+  const Range out = range(dx, n, i, lddx, b), rr = range(res, n, i, ldr, b);
+  if (meet_any(out, range(dy, n, o, lddy, b), range(w, o, i, ldw, b))) return EF_EINVAL;
+  if (kept && meet_any(out, range_kept(codes, n, i), range_scales(scales, n, i))) return EF_EINVAL;
+  if (meet(out, rr) && !(res == dx && ldr == lddx)) return EF_EINVAL;
+  if (n == 0) return EF_OK;
+  Product p{n, i, o, {dy, lddy}, {w, ldw}, {},
+            {dx, lddx, nullptr, res, ldr, {const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), groups(i), fmt}, act, 0}};
+  return dtype == EF_F32 ? run_product<K_DGRAD, EF_F32, EF_F32>(p, S(stream))
+                         : run_product<K_DGRAD, EF_BF16, EF_BF16>(p, S(stream));
+}
+
+int ef_linear_wgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t lddy, int dtype, const uint8_t* codes,
+                    const uint8_t* scales, int fmt, void* dw, void* db, int g_dtype, int accumulate, void* ws,
+                    size_t ws_bytes, void* stream) {
+  EF_TRY(check_sizes(n, i, o));
+  if (!dtype_ok(dtype) || !dtype_ok(g_dtype) || !fmt_ok(fmt) || !mat_ok(dy, n, o, lddy, dtype) ||
+      !kept_ok(codes, scales, n) || !dw || !aligned(dw, (size_t)bytes_of(g_dtype)) ||
+      (db && !aligned(db, (size_t)bytes_of(g_dtype))) || (accumulate && g_dtype != EF_F32))
+    return EF_EINVAL;
+  const int64_t b = bytes_of(g_dtype);
+  const Range rw = range(dw, o, i, i, b), rb = range(db, 1, o, o, b), ry = range(dy, n, o, lddy, bytes_of(dtype)),
+              q = range_kept(codes, n, i), s = range_scales(scales, n, i);
+  if (meet_any(rw, rb, ry, q, s) || meet_any(rb, ry, q, s)) return EF_EINVAL;
+  hipStream_t st = S(stream);
+  Product p{o, i, n, {dy, lddy}, {}, {const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), groups(i), fmt},
+            {dw, i, nullptr, nullptr, 0, {}, EF_ACT_NONE, accumulate ? 1 : 0}};
+  if (dtype == EF_F32) {
+    if (g_dtype == EF_F32) EF_TRY((run_product<K_WGRAD, EF_F32, EF_F32>(p, st)));
+    else EF_TRY((run_product<K_WGRAD, EF_F32, EF_BF16>(p, st)));
+  } else {
+    if (g_dtype == EF_F32) EF_TRY((run_product<K_WGRAD, EF_BF16, EF_F32>(p, st)));
+    else EF_TRY((run_product<K_WGRAD, EF_BF16, EF_BF16>(p, st)));
+  }
+  if (!db) return EF_OK;
+  const dim3 grid((unsigned)((o + 31) / 32)), blk(256);
+  const int add = accumulate ? 1 : 0;
+  if (dtype == EF_F32) {
+    if (g_dtype == EF_F32) EF_LAUNCH((k_bias_grad<EF_F32, EF_F32>), grid, blk, 0, st, n, (int32_t)o, dy, lddy, db, add);
+    else EF_LAUNCH((k_bias_grad<EF_F32, EF_BF16>), grid, blk, 0, st, n, (int32_t)o, dy, lddy, db, add);
+  } else {
+    if (g_dtype == EF_F32) EF_LAUNCH((k_bias_grad<EF_BF16, EF_F32>), grid, blk, 0, st, n, (int32_t)o, dy, lddy, db, add);
+    else EF_LAUNCH((k_bias_grad<EF_BF16, EF_BF16>), grid, blk, 0, st, n, (int32_t)o, dy, lddy, db, add);
+  }
+  return launched();
+}
+
+}  // extern "C"

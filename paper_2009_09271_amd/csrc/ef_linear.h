@@ -436,6 +436,354 @@ __global__ __launch_bounds__(256) void k_linear_any(int32_t M, int32_t N, int32_
   }
 }
 
+// ---------------------------------------------------------------------------------------------
+// The same products on bfloat16 matrix instructions, for matrices whose rows start on 16 bytes.
+//
+// A workgroup has BM x BN of C, WM x WN wavefronts, and steps of 64 along k through two halves of the LDS.  A
+// wavefront has BM / WM rows and 64 columns of C in accumulators of 32 x 32.  Operands go from memory to the LDS
+// without passing registers (16 bytes a lane; what lies outside the matrix arrives as zeros by the buffer's
+// bounds), in the order that they have in memory:
+//   k along the row   [line][64]: 16-byte chunk c of line r at place c ^ (r & 7), so that eight lines' reads of
+//                     one k fall on different banks; read 16 bytes a lane
+//   k down the rows   [64][line]: 64-byte unit u of row k at place u ^ (k & 3), so that four rows' reads do; read
+//                     by the transposing load, which hands four k of one line to a lane
+//   checkpoint        as k down the rows: its codes pass through registers, where they become bfloat16
+// A step's last fragments are read before the barrier that releases its half, and the next step's first ones
+// after it, ahead of the last fragments' instructions: the matrix pipes have work while the LDS changes hands.
+// ---------------------------------------------------------------------------------------------
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+#define EF_LDS __attribute__((address_space(3)))
+
+constexpr int kBK = 64;                    // k per step
+constexpr int kFar = 0x7FFFFFF0;           // a byte offset outside every buffer: reads give zeros
+constexpr int64_t kFastLd = (int64_t)1 << 21;  // leading dimensions up to this keep a tile's offsets in 31 bits
+
+// (the host pass does not know the buffer type)
+#if defined(__HIP_DEVICE_COMPILE__)
+#define EF_BUFFER(P, BYTES) __builtin_amdgcn_make_buffer_rsrc((void*)(P), 0, (int)(BYTES), 0x00020000)
+#define EF_BUFFER_TO_LDS(R, LDS, OFF) __builtin_amdgcn_raw_ptr_buffer_load_lds(R, (EF_LDS void*)(LDS), 16, OFF, 0, 0, 0)
+#define EF_BUFFER_B64(R, OFF) __builtin_amdgcn_raw_buffer_load_b64(R, OFF, 0, 0)
+#define EF_BUFFER_B8(R, OFF) __builtin_amdgcn_raw_buffer_load_b8(R, OFF, 0, 0)
+#else
+#define EF_BUFFER(P, BYTES) (BYTES)
+#define EF_BUFFER_TO_LDS(R, LDS, OFF) ((void)(R), (void)(OFF))
+#define EF_BUFFER_B64(R, OFF) (u32x2{(uint32_t)(R), 0u})
+#define EF_BUFFER_B8(R, OFF) ((uint32_t)(R))
+#endif
+
+// One operand's way into the LDS.  KC: k along the row.  LINES rows of C (or columns) per tile, NW wavefronts.
+template <bool KC, int LINES, int NW>
+struct Stream {
+  static constexpr int J = LINES * kBK * 2 / 1024 / NW;  // 1024 bytes per wavefront and load
+  const char* base;
+  int64_t step;   // bytes from one step to the next
+  int64_t ld2;
+  int64_t left;   // KC: bytes from base to the end of the matrix's last line; else bytes of a row from base on
+  int64_t K;
+  int off[J];
+  int chunk8;     // KC: first k of this lane's chunk
+
+  __device__ __forceinline__ void init(const Mat& m, int64_t line0, int64_t lines, int64_t k, int wave, int lane) {
+    ld2 = m.ld * 2;
+    K = k;
+    if (KC) {
+      base = static_cast<const char*>(m.p) + line0 * ld2;
+      step = kBK * 2;
+      const int64_t have = lines - line0 < LINES ? lines - line0 : LINES;
+      left = (have - 1) * ld2 + k * 2;
+      chunk8 = ((lane & 7) ^ (lane >> 3)) * 8;
+#pragma unroll
+      for (int j = 0; j < J; ++j) off[j] = ((j * NW + wave) * 8 + (lane >> 3)) * (int)ld2 + chunk8 * 2;
+    } else {
+      constexpr int CH = LINES / 8, R = 64 / CH;  // chunks per row, rows per load
+      base = static_cast<const char*>(m.p) + line0 * 2;
+      step = kBK * ld2;
+      left = (lines - line0) * 2;
+      chunk8 = 0;
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int row = (j * NW + wave) * R + lane / CH, chunk = (lane % CH) ^ ((row & 3) << 2);
+        off[j] = chunk * 16 < left ? row * (int)ld2 + chunk * 16 : kFar;
+      }
+    }
+  }
+
+  // the tile of step s into lds (LINES * 128 bytes)
+  __device__ __forceinline__ void load(int64_t s, char* lds, int wave) const {
+    const int64_t kleft = K - s * kBK;
+    const int64_t limit = KC ? left - s * step : ((kleft < kBK ? kleft : kBK) - 1) * ld2 + left;
+    const auto r = EF_BUFFER(base + s * step, limit);
+    const bool in = !KC || chunk8 < kleft;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+      EF_BUFFER_TO_LDS(r, lds + (j * NW + wave) * 1024, in ? off[j] : kFar);
+  }
+};
+
+// A checkpoint's way: NT threads, LINES columns per tile; eight codes a chunk.
+template <int LINES, int NT>
+struct StreamKept {
+  static constexpr int J = kBK * LINES / 8 / NT;
+  const uint8_t *codes, *scales;
+  int64_t K;
+  int32_t row_bytes, G, fmt, left;
+  int off[J], soff[J], to[J];
+  u32x2 q[J];
+  uint32_t s[J];
+
+  __device__ __forceinline__ void init(const Kept& k, int64_t line0, int64_t rows, int tid) {
+    row_bytes = k.G * kGroup;
+    G = k.G;
+    fmt = k.fmt;
+    K = rows;
+    codes = k.codes + line0;
+    scales = k.scales + line0 / kGroup;
+    left = row_bytes - (int32_t)line0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int id = j * NT + tid, row = id / (LINES / 8), c = id % (LINES / 8);
+      const bool in = c * 8 < left;
+      off[j] = in ? row * row_bytes + c * 8 : kFar;
+      soff[j] = in ? row * G + c / 4 : kFar;
+      to[j] = row * LINES * 2 + (((c >> 2) ^ (row & 3)) << 6) + (c & 3) * 16;
+    }
+  }
+  __device__ __forceinline__ void fetch(int64_t step) {
+    const int64_t k0 = step * kBK;
+    const int rows = K - k0 < kBK ? (int)(K - k0) : kBK;
+    const auto rc = EF_BUFFER(codes + k0 * row_bytes, (rows - 1) * row_bytes + left);
+    const auto rs = EF_BUFFER(scales + k0 * G, (rows - 1) * G + left / kGroup);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      q[j] = EF_BUFFER_B64(rc, off[j]);
+      s[j] = EF_BUFFER_B8(rs, soff[j]);
+    }
+  }
+  __device__ __forceinline__ void store(char* lds) const {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      u32x4 w;
+      if (fmt == EF_CKPT_INT8) {
+        float v[8];
+        decode8(q[j], s[j], EF_CKPT_INT8, v);
+#pragma unroll
+        for (int h = 0; h < 4; ++h)  // (exact: the low halves are zeros)
+          w[h] = __builtin_amdgcn_perm(__float_as_uint(v[2 * h + 1]), __float_as_uint(v[2 * h]), 0x07060302u);
+      } else {
+        const float r = __uint_as_float(s[j] << 23);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          w[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[j][h], r, false));
+          w[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[j][h], r, true));
+        }
+      }
+      *reinterpret_cast<u32x4*>(lds + to[j]) = w;
+    }
+  }
+};
+
+// A wavefront's fragments of one operand: T of 32 lines by 16 k, eight k a lane.
+template <bool KC, int LINES, int T>
+struct Reader {
+  int off[KC ? 4 : T];
+  __device__ __forceinline__ void init(int line0, int lane) {
+    if (KC) {
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+        off[ks] = (line0 + (lane & 31)) * 128 + (((ks * 2 + (lane >> 5)) ^ (lane & 7)) << 4);
+    } else {
+      const int x = (lane >> 2) & 3;
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+        off[t] = ((lane >> 5) * 8 + x) * LINES * 2 + (((line0 / 32 + t) ^ x) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    }
+  }
+  __device__ __forceinline__ void read(const char* lds, int ks, bf16x8 (&f)[T]) const {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      if (KC) {
+        f[t] = *reinterpret_cast<const bf16x8*>(lds + off[ks] + t * 32 * 128);
+      } else {
+        const char* p = lds + off[t] + ks * 16 * LINES * 2;
+        const bf16x4 a = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((EF_LDS s16x4*)p));
+        const bf16x4 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((EF_LDS s16x4*)(p + 4 * LINES * 2)));
+        f[t] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    }
+  }
+};
+
+// Tiles in an order in which those that run at one time on an XCD (workgroups b, b + 8, b + 16, ...) are
+// neighbours: each XCD has a run of the tiles, in bands of eight rows of tiles.
+__device__ __forceinline__ void tile_of(uint32_t b, uint32_t tm, uint32_t tn, uint32_t* m, uint32_t* n) {
+  const uint32_t T = tm * tn, q = T / 8, rest = T % 8, x = b % 8;
+  const uint32_t id = x * q + (x < rest ? x : rest) + b / 8;
+  const uint32_t band = id / (8 * tn), h = tm - band * 8 < 8 ? tm - band * 8 : 8, in = id - band * 8 * tn;
+  *m = band * 8 + in % h;
+  *n = in / h;
+}
+
+// The sums of a split product: partial [split][M][Np] floats, Np = N rounded up to a group.
+struct Split {
+  float* part;
+  int64_t plane;   // M * Np
+  int32_t Np;
+  int32_t per;     // steps per split
+};
+
+template <int KIND, int DO, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32_t N, int32_t K, Mat A, Mat B, Kept BK, Epi ep, Split sp) {
+  constexpr bool AKC = KIND != K_WGRAD, BKC = KIND == K_FWD, B8 = KIND == K_WGRAD;
+  constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+  static_assert(TN == 2, "the epilogue hands over 64 columns a wavefront");
+  constexpr int kA = BM * kBK * 2, kHalf = (BM + BN) * kBK * 2;
+  __shared__ __align__(1024) char lds[2 * kHalf];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  uint32_t ti, tj;
+  tile_of(blockIdx.x, ((uint32_t)M + BM - 1) / BM, ((uint32_t)N + BN - 1) / BN, &ti, &tj);
+  const int64_t m0 = (int64_t)ti * BM, n0 = (int64_t)tj * BN;
+  const int wm = wave / WN * (BM / WM), wn = wave % WN * 64;
+  const int64_t all = ((int64_t)K + kBK - 1) / kBK;
+  const int64_t s0 = (int64_t)blockIdx.y * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
+
+  Stream<AKC, BM, NW> sa;
+  sa.init(A, m0, M, K, wave, lane);
+  Stream<BKC, BN, NW> sb;
+  StreamKept<BN, NW * 64> sk;
+  if (B8) sk.init(BK, n0, K, tid);
+  else sb.init(B, n0, N, K, wave, lane);
+  Reader<AKC, BM, TM> ra;
+  Reader<BKC, BN, TN> rb;
+  ra.init(wm, lane);
+  rb.init(wn, lane);
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int a = 0; a < TM; ++a)
+#pragma unroll
+    for (int b = 0; b < TN; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.0f;
+  bf16x8 fa[2][TM], fb[2][TN];
+  auto mul = [&](int h) {
+#pragma unroll
+    for (int a = 0; a < TM; ++a)
+#pragma unroll
+      for (int b = 0; b < TN; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[h][a], fb[h][b], acc[a][b], 0, 0, 0);
+  };
+
+  sa.load(s0, lds, wave);
+  if (B8) {
+    sk.fetch(s0);
+    sk.store(lds + kA);
+  } else {
+    sb.load(s0, lds + kA, wave);
+  }
+  if (s0 + 1 < s1) {
+    sa.load(s0 + 1, lds + kHalf, wave);
+    if (B8) {
+      sk.fetch(s0 + 1);
+      sk.store(lds + kHalf + kA);
+      if (s0 + 2 < s1) sk.fetch(s0 + 2);
+    } else {
+      sb.load(s0 + 1, lds + kHalf + kA, wave);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  ra.read(lds, 0, fa[0]);
+  rb.read(lds + kA, 0, fb[0]);
+  char* cur = lds;
+  char* nxt = lds + kHalf;
+  auto slices = [&]() {
+#pragma unroll
+    for (int ks = 0; ks < 3; ++ks) {
+      ra.read(cur, ks + 1, fa[(ks + 1) & 1]);
+      rb.read(cur + kA, ks + 1, fb[(ks + 1) & 1]);
+      mul(ks & 1);
+    }
+  };
+  for (int64_t s = s0; s + 1 < s1; ++s) {
+    slices();
+    __builtin_amdgcn_s_waitcnt(0);  // this wavefront's part of the next step has arrived, its last reads are done
+    __syncthreads();
+    if (s + 2 < s1) {
+      sa.load(s + 2, cur, wave);
+      if (B8) {
+        sk.store(cur + kA);
+        if (s + 3 < s1) sk.fetch(s + 3);
+      } else {
+        sb.load(s + 2, cur + kA, wave);
+      }
+    }
+    ra.read(nxt, 0, fa[0]);
+    rb.read(nxt + kA, 0, fb[0]);
+    mul(1);
+    char* x = cur;
+    cur = nxt;
+    nxt = x;
+  }
+  slices();
+  mul(1);
+  __syncthreads();
+  // as in k_linear_any: through the LDS, 32 rows of a wavefront at a time
+  float* slab = reinterpret_cast<float*>(lds) + wave * 32 * kSlabPitch;
+#pragma unroll
+  for (int a = 0; a < TM; ++a) {
+#pragma unroll
+    for (int b = 0; b < TN; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        slab[((r >> 2) * 8 + (lane >> 5) * 4 + (r & 3)) * kSlabPitch + b * 32 + (lane & 31)] = acc[a][b][r];
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int rr = q * 8 + (lane >> 3), cc = (lane & 7) * 8;
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(slab + rr * kSlabPitch + cc);
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(slab + rr * kSlabPitch + cc + 4);
+      const int64_t row = m0 + wm + a * 32 + rr;
+      const int32_t col = (int32_t)(n0 + wn + cc);
+      if (sp.part) {
+        if (row < M && col < sp.Np) {
+          float* p = sp.part + blockIdx.y * sp.plane + row * sp.Np + col;
+          *reinterpret_cast<f32x4*>(p) = lo;
+          *reinterpret_cast<f32x4*>(p + 4) = hi;
+        }
+      } else {
+        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        epilogue8<KIND, DO>(ep, row, col, row < M, N, v);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// The splits' sums in order, then the epilogue.  Np / 8 lanes a row, whole groups side by side.
+template <int KIND, int DO>
+__global__ __launch_bounds__(256) void k_linear_join(int32_t M, int32_t N, int splits, Split sp, Epi ep) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int32_t w = sp.Np / 8;
+  const int64_t row = id / w;
+  const int32_t col = (int32_t)(id - row * w) * 8;
+  const bool in = row < M;
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (in)
+    for (int z = 0; z < splits; ++z) {
+      const float* p = sp.part + z * sp.plane + row * sp.Np + col;
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] += lo[j];
+        v[j + 4] += hi[j];
+      }
+    }
+  epilogue8<KIND, DO>(ep, row, col, in, N, v);
+}
+
 // The bias gradient: db[o] (+)= sum over the rows of dy[., o], in float32: a workgroup has 32 columns, eight
 // lanes down, each lane's rows in order, the eight sums in order.
 template <int DT, int DO>

@@ -74,8 +74,35 @@ int check_sizes(int64_t n, int64_t i, int64_t o) {
   return EF_OK;
 }
 
+// bfloat16 matrices whose rows start on 16 bytes and hold whole 16-byte chunks
+bool fast_mat(const Mat& m, int64_t cols) {
+  return aligned(m.p, 16) && m.ld % 8 == 0 && cols % 8 == 0 && m.ld <= kFastLd;
+}
+
+template <int KIND>
+bool fast_ok(const Product& p) {
+  if (p.K == 0 || !fast_mat(p.A, KIND == K_WGRAD ? p.M : p.K)) return false;
+  return KIND == K_WGRAD ? p.N <= kFastLd : fast_mat(p.B, KIND == K_FWD ? p.K : p.N);
+}
+
+template <int KIND, int DO, int BM, int BN, int WM, int WN>
+int run_fast(const Product& p, hipStream_t st) {
+  const int64_t tiles = ((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN), steps = (p.K + kBK - 1) / kBK;
+  if (tiles > kMaxGrid) return EF_ERANGE;
+  const Split sp{nullptr, 0, 0, (int32_t)steps};
+  EF_LAUNCH((k_linear_bf16<KIND, DO, BM, BN, WM, WN>), dim3((unsigned)tiles, 1), dim3(WM * WN * 64), 0, st, (int32_t)p.M,
+            (int32_t)p.N, (int32_t)p.K, p.A, p.B, p.BK, p.ep, sp);
+  return launched();
+}
+
 template <int KIND, int DT, int DO>
 int run_product(const Product& p, hipStream_t st) {
+  if constexpr (DT == EF_BF16) {
+    if (fast_ok<KIND>(p)) {
+      if (((p.M + 255) / 256) * ((p.N + 255) / 256) >= 192) return run_fast<KIND, DO, 256, 256, 2, 4>(p, st);
+      return run_fast<KIND, DO, 128, 128, 2, 2>(p, st);
+    }
+  }
   const int64_t tiles = ((p.M + kAnyTile - 1) / kAnyTile) * ((p.N + kAnyTile - 1) / kAnyTile);
   if (tiles > kMaxGrid) return EF_ERANGE;
   EF_LAUNCH((k_linear_any<KIND, DT, DO>), dim3((unsigned)tiles), dim3(256), 0, st, (int32_t)p.M, (int32_t)p.N,

@@ -272,7 +272,8 @@ struct Epi {
   int64_t ldr;
   Kept k;             // forward: written where codes is not null; dgrad: read where act is not EF_ACT_NONE
   int32_t act;
-  int32_t add;        // wgrad: dw += product
+  int32_t add;        // wgrad: dw += product, db += sum
+  void* db;           // wgrad: [M], the sums of A's lines, or null
 };
 
 // KIND the product, DT the type of out, bias and res.
@@ -324,6 +325,73 @@ __device__ __forceinline__ void epilogue8(const Epi& a, int64_t row, int32_t col
   store8<DT>(a.out, row * a.ldo + col, cnt, v);
 }
 
+template <int DO>
+__device__ __forceinline__ void store_db(const Epi& a, int64_t m, float s) {
+  if (DO == EF_F32) {
+    float* q = static_cast<float*>(a.db) + m;
+    *q = a.add ? *q + s : s;
+  } else {
+    static_cast<uint16_t*>(a.db)[m] = (uint16_t)f_bf16x2(s, 0.0f);
+  }
+}
+
+// The sums of a product whose k is split over workgroups: partial C [split][M][Np] floats, Np = N rounded up to
+// a group, then (wgrad) partial db [split][M].
+struct Split {
+  float* part;     // null: not split
+  float* part_db;
+  int64_t plane;   // M * Np
+  int32_t Np;
+  int32_t per;     // steps per split
+};
+
+// A wavefront's 32 x 64 of C, handed over through its part of the LDS: from lanes that hold single columns (four
+// rows each) to lanes that hold eight columns of a row.  Every wavefront of the workgroup takes part.
+constexpr int kSlabPitch = 68;
+template <int KIND, int DO>
+__device__ __forceinline__ void finish(const f32x16 (&acc)[2], float* slab, int lane, int64_t row0, int64_t col0, int32_t M,
+                                       int32_t N, const Epi& ep, const Split& sp) {
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      slab[((r >> 2) * 8 + (lane >> 5) * 4 + (r & 3)) * kSlabPitch + b * 32 + (lane & 31)] = acc[b][r];
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int rr = q * 8 + (lane >> 3), cc = (lane & 7) * 8;
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(slab + rr * kSlabPitch + cc);
+    const f32x4 hi = *reinterpret_cast<const f32x4*>(slab + rr * kSlabPitch + cc + 4);
+    const int64_t row = row0 + rr;
+    const int32_t col = (int32_t)(col0 + cc);
+    if (sp.part) {
+      if (row < M && col < sp.Np) {
+        float* p = sp.part + blockIdx.y * sp.plane + row * sp.Np + col;
+        *reinterpret_cast<f32x4*>(p) = lo;
+        *reinterpret_cast<f32x4*>(p + 4) = hi;
+      }
+    } else {
+      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      epilogue8<KIND, DO>(ep, row, col, row < M, N, v);
+    }
+  }
+  __syncthreads();
+}
+
+// wgrad, the wavefronts of the first column of tiles: the sums of A's lines that went by; two lanes hold a line.
+template <int DO, int T>
+__device__ __forceinline__ void finish_db(const float (&s)[T], int lane, int64_t m0, int32_t M, const Epi& ep, const Split& sp) {
+#pragma unroll
+  for (int a = 0; a < T; ++a) {
+    const float t = s[a] + __shfl_xor(s[a], 32);
+    const int64_t m = m0 + a * 32 + lane;
+    if (lane < 32 && m < M) {
+      if (sp.part) sp.part_db[(int64_t)blockIdx.y * M + m] = t;
+      else store_db<DO>(ep, m, t);
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------------------------
 // The product for every type, order and alignment, in float32: C[m][n] = sum_k A(m, k) B(n, k).
 //   forward  A = x  [n][i] (k along the row), B = W [o][i] (k along the row)
@@ -339,7 +407,6 @@ struct Mat {
 };
 
 constexpr int kAnyTile = 128, kAnyK = 16, kAnyPitch = 132;  // (132: rows eight apart land 32 banks apart)
-constexpr int kSlabPitch = 68;  // epilogue: a wavefront's 32 x 64 floats
 
 // Eight elements along the contiguous direction of a tile of A or B: ROWS of the matrix down, 8 columns across.
 template <int DT>
@@ -349,7 +416,7 @@ __device__ __forceinline__ void load_chunk(const Mat& a, int64_t row, int64_t ro
 }
 
 template <int KIND, int DT, int DO>
-__global__ __launch_bounds__(256) void k_linear_any(int32_t M, int32_t N, int32_t K, Mat A, Mat B, Kept BK, Epi ep) {
+__global__ __launch_bounds__(256) void k_linear_any(int32_t M, int32_t N, int32_t K, Mat A, Mat B, Kept BK, Epi ep, Split sp) {
   constexpr bool AKC = KIND != K_WGRAD, BKC = KIND == K_FWD, B8 = KIND == K_WGRAD;
   constexpr int kTileF = kAnyK * kAnyPitch;
   __shared__ __align__(16) float sm[4 * 32 * kSlabPitch > 4 * kTileF ? 4 * 32 * kSlabPitch : 4 * kTileF];
@@ -392,15 +459,18 @@ __global__ __launch_bounds__(256) void k_linear_any(int32_t M, int32_t N, int32_
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.0f;
-  const int steps = (int)(((int64_t)K + kAnyK - 1) / kAnyK);
-  if (steps) fetch(0);
-  for (int s = 0; s < steps; ++s) {
+  const bool sums = KIND == K_WGRAD && ep.db && n0 == 0 && wn == 0;
+  float bs[2] = {0.0f, 0.0f};
+  const int64_t all = ((int64_t)K + kAnyK - 1) / kAnyK;
+  const int64_t s0 = (int64_t)blockIdx.y * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
+  if (s0 < s1) fetch(s0 * kAnyK);
+  for (int64_t s = s0; s < s1; ++s) {
     float* sa = sm + (s & 1) * 2 * kTileF;
     float* sb = sa + kTileF;
     put(sa, AKC, av);
     put(sb, BKC, bv);
     __syncthreads();  // (the other half was last read before the previous barrier's step ended)
-    if (s + 1 < steps) fetch((int64_t)(s + 1) * kAnyK);
+    if (s + 1 < s1) fetch((s + 1) * kAnyK);
 #pragma unroll
     for (int k = 0; k < kAnyK; k += 2) {
       const int row = (k + (lane >> 5)) * kAnyPitch + (lane & 31);
@@ -409,31 +479,17 @@ __global__ __launch_bounds__(256) void k_linear_any(int32_t M, int32_t N, int32_
       acc[0][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a0, b1, acc[0][1], 0, 0, 0);
       acc[1][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a1, b0, acc[1][0], 0, 0, 0);
       acc[1][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a1, b1, acc[1][1], 0, 0, 0);
+      if (sums) {
+        bs[0] += a0;
+        bs[1] += a1;
+      }
     }
   }
   __syncthreads();
-  // a wavefront's 64 x 64 through its own part of the LDS, 32 rows at a time: lanes that hold single columns
-  // (four rows each) hand over to lanes that hold eight columns of a row
   float* slab = sm + wave * 32 * kSlabPitch;
 #pragma unroll
-  for (int a = 0; a < 2; ++a) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        slab[((r >> 2) * 8 + (lane >> 5) * 4 + (r & 3)) * kSlabPitch + b * 32 + (lane & 31)] = acc[a][b][r];
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int rr = q * 8 + (lane >> 3), cc = (lane & 7) * 8;
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(slab + rr * kSlabPitch + cc);
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(slab + rr * kSlabPitch + cc + 4);
-      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      const int64_t row = m0 + wm + a * 32 + rr;
-      epilogue8<KIND, DO>(ep, row, (int32_t)(n0 + wn + cc), row < M, N, v);
-    }
-    __syncthreads();
-  }
+  for (int a = 0; a < 2; ++a) finish<KIND, DO>(acc[a], slab, lane, m0 + wm + a * 32, n0 + wn, M, N, ep, sp);
+  if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -466,11 +522,13 @@ constexpr int64_t kFastLd = (int64_t)1 << 21;  // leading dimensions up to this 
 #if defined(__HIP_DEVICE_COMPILE__)
 #define EF_BUFFER(P, BYTES) __builtin_amdgcn_make_buffer_rsrc((void*)(P), 0, (int)(BYTES), 0x00020000)
 #define EF_BUFFER_TO_LDS(R, LDS, OFF) __builtin_amdgcn_raw_ptr_buffer_load_lds(R, (EF_LDS void*)(LDS), 16, OFF, 0, 0, 0)
+#define EF_BUFFER_B128(R, OFF) __builtin_amdgcn_raw_buffer_load_b128(R, OFF, 0, 0)
 #define EF_BUFFER_B64(R, OFF) __builtin_amdgcn_raw_buffer_load_b64(R, OFF, 0, 0)
 #define EF_BUFFER_B8(R, OFF) __builtin_amdgcn_raw_buffer_load_b8(R, OFF, 0, 0)
 #else
 #define EF_BUFFER(P, BYTES) (BYTES)
 #define EF_BUFFER_TO_LDS(R, LDS, OFF) ((void)(R), (void)(OFF))
+#define EF_BUFFER_B128(R, OFF) (u32x4{(uint32_t)(R), (uint32_t)(OFF), 0u, 0u})
 #define EF_BUFFER_B64(R, OFF) (u32x2{(uint32_t)(R), 0u})
 #define EF_BUFFER_B8(R, OFF) ((uint32_t)(R))
 #endif
@@ -617,6 +675,14 @@ struct Reader {
   }
 };
 
+// s plus the eight elements of a fragment, in float32 (two at a time against ones)
+__device__ __forceinline__ float add8(bf16x8 f, float s) {
+  const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{f[2 * j], f[2 * j + 1]}, one, s, false);
+  return s;
+}
+
 // Tiles in an order in which those that run at one time on an XCD (workgroups b, b + 8, b + 16, ...) are
 // neighbours: each XCD has a run of the tiles, in bands of eight rows of tiles.
 __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tm, uint32_t tn, uint32_t* m, uint32_t* n) {
@@ -626,14 +692,6 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tm, uint32_t tn, ui
   *m = band * 8 + in % h;
   *n = in / h;
 }
-
-// The sums of a split product: partial [split][M][Np] floats, Np = N rounded up to a group.
-struct Split {
-  float* part;
-  int64_t plane;   // M * Np
-  int32_t Np;
-  int32_t per;     // steps per split
-};
 
 template <int KIND, int DO, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32_t N, int32_t K, Mat A, Mat B, Kept BK, Epi ep, Split sp) {
@@ -668,12 +726,20 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
     for (int b = 0; b < TN; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.0f;
+  const bool sums = KIND == K_WGRAD && ep.db && n0 == 0 && wn == 0;
+  float bs[TM];
+#pragma unroll
+  for (int a = 0; a < TM; ++a) bs[a] = 0.0f;
   bf16x8 fa[2][TM], fb[2][TN];
   auto mul = [&](int h) {
 #pragma unroll
     for (int a = 0; a < TM; ++a)
 #pragma unroll
       for (int b = 0; b < TN; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[h][a], fb[h][b], acc[a][b], 0, 0, 0);
+    if (sums) {
+#pragma unroll
+      for (int a = 0; a < TM; ++a) bs[a] = add8(fa[h][a], bs[a]);
+    }
   };
 
   sa.load(s0, lds, wave);
@@ -730,36 +796,79 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
   slices();
   mul(1);
   __syncthreads();
-  // as in k_linear_any: through the LDS, 32 rows of a wavefront at a time
   float* slab = reinterpret_cast<float*>(lds) + wave * 32 * kSlabPitch;
 #pragma unroll
-  for (int a = 0; a < TM; ++a) {
+  for (int a = 0; a < TM; ++a) finish<KIND, DO>(acc[a], slab, lane, m0 + wm + a * 32, n0 + wn, M, N, ep, sp);
+  if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
+}
+
+// ---------------------------------------------------------------------------------------------
+// The forward product of a few tokens (up to 16 TT): the weights are read once, and that bounds it.  A workgroup
+// has 16 OT output features and splits k over its eight wavefronts; each takes the weights' rows as the first
+// operand and the tokens as the second, straight from memory to registers, 16 bytes a lane, eight loads of the
+// weights in flight.  The eight partial sums are added in order through the LDS.
+// ---------------------------------------------------------------------------------------------
+constexpr int kFewWaves = 8;
+constexpr int kFewTokens = 32;
+
+template <int TT, int OT>
+__global__ __launch_bounds__(kFewWaves * 64) void k_linear_few(int32_t n, int32_t N, int32_t K, Mat X, Mat W, Epi ep) {
+  __shared__ f32x4 red[kFewWaves][TT][OT][64];
+  constexpr int U = 8 / OT;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t o0 = (int64_t)blockIdx.x * 16 * OT;
+  const int64_t ldw = W.ld * 2, ldx = X.ld * 2;
+  const int64_t have = N - o0 < 16 * OT ? N - o0 : 16 * OT;
+  const auto rw = EF_BUFFER(static_cast<const char*>(W.p) + o0 * ldw, (have - 1) * ldw + (int64_t)K * 2);
+  const auto rx = EF_BUFFER(X.p, (int64_t)(n - 1) * ldx + (int64_t)K * 2);
+  const int kl = (lane >> 4) * 8;
+  const int per = ((K + 32 * kFewWaves - 1) / (32 * kFewWaves) + 3) / 4 * 4;  // steps of 32 per wavefront: whole 256-byte runs
+  const int c0 = wave * per, c1 = c0 + per;
+  f32x4 acc[TT][OT];
 #pragma unroll
-    for (int b = 0; b < TN; ++b)
+  for (int t = 0; t < TT; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        slab[((r >> 2) * 8 + (lane >> 5) * 4 + (r & 3)) * kSlabPitch + b * 32 + (lane & 31)] = acc[a][b][r];
-    __syncthreads();
+    for (int o = 0; o < OT; ++o) acc[t][o] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int c = c0; c < c1 && c * 32 < K; c += U) {
+    u32x4 w[U][OT], x[U][TT];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int rr = q * 8 + (lane >> 3), cc = (lane & 7) * 8;
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(slab + rr * kSlabPitch + cc);
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(slab + rr * kSlabPitch + cc + 4);
-      const int64_t row = m0 + wm + a * 32 + rr;
-      const int32_t col = (int32_t)(n0 + wn + cc);
-      if (sp.part) {
-        if (row < M && col < sp.Np) {
-          float* p = sp.part + blockIdx.y * sp.plane + row * sp.Np + col;
-          *reinterpret_cast<f32x4*>(p) = lo;
-          *reinterpret_cast<f32x4*>(p + 4) = hi;
-        }
-      } else {
-        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        epilogue8<KIND, DO>(ep, row, col, row < M, N, v);
-      }
+    for (int u = 0; u < U; ++u) {
+      const int k = (c + u) * 32 + kl;
+      const bool in = k < K && c + u < c1;
+#pragma unroll
+      for (int o = 0; o < OT; ++o) w[u][o] = EF_BUFFER_B128(rw, in ? (int)((o * 16 + (lane & 15)) * ldw) + k * 2 : kFar);
+#pragma unroll
+      for (int t = 0; t < TT; ++t) x[u][t] = EF_BUFFER_B128(rx, in ? (int)((t * 16 + (lane & 15)) * ldx) + k * 2 : kFar);
     }
-    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int o = 0; o < OT; ++o)
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+          acc[t][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[u][o]), __builtin_bit_cast(bf16x8, x[u][t]),
+                                                             acc[t][o], 0, 0, 0);
   }
+#pragma unroll
+  for (int t = 0; t < TT; ++t)
+#pragma unroll
+    for (int o = 0; o < OT; ++o) red[wave][t][o][lane] = acc[t][o];
+  __syncthreads();
+  // eight outputs of a token per lane; four neighbouring lanes a group where OT is 2
+  if (tid >= TT * 16 * OT * 2) return;
+  const int q = tid % (OT * 2), token = tid / (OT * 2);
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+  for (int z = 0; z < kFewWaves; ++z) {
+    const f32x4* p = red[z][token >> 4][q >> 1] + (q & 1) * 32 + (token & 15);
+    const f32x4 lo = p[0], hi = p[16];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[j] += lo[j];
+      v[j + 4] += hi[j];
+    }
+  }
+  epilogue8<K_FWD, EF_BF16>(ep, token, (int32_t)o0 + q * 8, token < n, N, v);
 }
 
 // The splits' sums in order, then the epilogue.  Np / 8 lanes a row, whole groups side by side.
@@ -770,6 +879,14 @@ __global__ __launch_bounds__(256) void k_linear_join(int32_t M, int32_t N, int s
   const int64_t row = id / w;
   const int32_t col = (int32_t)(id - row * w) * 8;
   const bool in = row < M;
+  if (KIND == K_WGRAD && !in) {  // the lanes behind the last row: db
+    const int64_t m = id - (int64_t)M * w;
+    if (!ep.db || m >= M) return;
+    float t = 0.0f;
+    for (int z = 0; z < splits; ++z) t += sp.part_db[(int64_t)z * M + m];
+    store_db<DO>(ep, m, t);
+    return;
+  }
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   if (in)
     for (int z = 0; z < splits; ++z) {
@@ -782,32 +899,6 @@ __global__ __launch_bounds__(256) void k_linear_join(int32_t M, int32_t N, int s
       }
     }
   epilogue8<KIND, DO>(ep, row, col, in, N, v);
-}
-
-// The bias gradient: db[o] (+)= sum over the rows of dy[., o], in float32: a workgroup has 32 columns, eight
-// lanes down, each lane's rows in order, the eight sums in order.
-template <int DT, int DO>
-__global__ __launch_bounds__(256) void k_bias_grad(int64_t n, int32_t o, const void* dy, int64_t ld, void* db, int add) {
-  __shared__ float part[8][32];
-  const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
-  const int64_t col = (int64_t)blockIdx.x * 32 + c;
-  float s = 0.0f;
-  if (col < o)
-    for (int64_t row = r; row < n; row += 8)
-      s += DT == EF_F32 ? static_cast<const float*>(dy)[row * ld + col]
-                        : bf16_f(static_cast<const uint16_t*>(dy)[row * ld + col]);
-  part[r][c] = s;
-  __syncthreads();
-  if (r == 0 && col < o) {
-#pragma unroll
-    for (int j = 1; j < 8; ++j) s += part[j][c];
-    if (DO == EF_F32) {
-      float* q = static_cast<float*>(db) + col;
-      *q = add ? *q + s : s;
-    } else {
-      static_cast<uint16_t*>(db)[col] = (uint16_t)f_bf16x2(s, 0.0f);
-    }
-  }
 }
 
 }  // namespace efs

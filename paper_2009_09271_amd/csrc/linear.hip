@@ -5,6 +5,7 @@
 #include "ef_linear.h"
 
 #include <algorithm>
+#include <cmath>
 
 using namespace efs;
 
@@ -85,28 +86,107 @@ bool fast_ok(const Product& p) {
   return KIND == K_WGRAD ? p.N <= kFastLd : fast_mat(p.B, KIND == K_FWD ? p.K : p.N);
 }
 
-template <int KIND, int DO, int BM, int BN, int WM, int WN>
-int run_fast(const Product& p, hipStream_t st) {
-  const int64_t tiles = ((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN), steps = (p.K + kBK - 1) / kBK;
-  if (tiles > kMaxGrid) return EF_ERANGE;
-  const Split sp{nullptr, 0, 0, (int32_t)steps};
-  EF_LAUNCH((k_linear_bf16<KIND, DO, BM, BN, WM, WN>), dim3((unsigned)tiles, 1), dim3(WM * WN * 64), 0, st, (int32_t)p.M,
-            (int32_t)p.N, (int32_t)p.K, p.A, p.B, p.BK, p.ep, sp);
-  return launched();
+// How a product is run: over `splits` parts of k, `per` steps each (the last may have fewer), whose sums are joined.
+enum Form { kAny, kSmall, kLarge };  // k_linear_any, k_linear_bf16 of 128 x 128, of 256 x 256
+struct Plan {
+  Form form;
+  int32_t splits, per;
+};
+
+constexpr int kCUs = 256;
+
+// Microseconds that a form takes, from what was measured: `step` for one step along k of the workgroups that a CU
+// holds (one of 256 x 256 or of k_linear_any; two of 128 x 128, `half` where it holds one), `fixed` for its start
+// and its epilogue; joining: a launch, and the partial sums written and read.
+struct Cost {
+  int tile, k, per_cu;
+  double step, half, fixed;
+};
+constexpr Cost kCosts[3] = {{kAnyTile, kAnyK, 1, 0.9, 0.9, 4.0}, {128, kBK, 2, 0.75, 0.45, 4.0}, {256, kBK, 1, 1.3, 1.3, 6.0}};
+
+double cost_of(const Cost& c, int64_t M, int64_t N, int64_t K, int64_t splits, int64_t per) {
+  const double wgs = (double)((M + c.tile - 1) / c.tile) * (double)((N + c.tile - 1) / c.tile) * (double)splits;
+  const double rounds = std::ceil(wgs / (kCUs * c.per_cu));
+  double t = rounds * ((wgs <= kCUs ? c.half : c.step) * (double)per + c.fixed);
+  if (splits > 1) t += 4.0 + (double)splits * (double)M * (double)N * 8.0 / 4.5e6;
+  return t;
+}
+
+// The form and the number of splits that these costs are least for.  The choice goes by sizes and alignment alone:
+// the same call always sums in the same order.
+Plan plan_of(bool fast, int64_t M, int64_t N, int64_t K) {
+  Plan best{kAny, 1, 1};
+  double least = 0.0;
+  for (int f = fast ? kSmall : kAny; f <= (fast ? kLarge : kAny); ++f) {
+    const Cost& c = kCosts[f];
+    const int64_t steps = std::max<int64_t>((K + c.k - 1) / c.k, 1);
+    const int64_t tiles = ((M + c.tile - 1) / c.tile) * ((N + c.tile - 1) / c.tile);
+    for (int64_t s = 1; s <= 64 && s <= steps && (s == 1 || tiles * s <= 2 * kCUs * c.per_cu); ++s) {
+      const int64_t per = (steps + s - 1) / s, splits = (steps + per - 1) / per;
+      if (splits != s) continue;
+      const double t = cost_of(c, M, N, K, splits, per);
+      if (least == 0.0 || t < least) {
+        least = t;
+        best = {(Form)f, (int32_t)splits, (int32_t)per};
+      }
+    }
+  }
+  return best;
+}
+
+int32_t padded(int64_t N) { return groups(N) * kGroup; }
+
+// The workspace of a product, whatever the alignment of its matrices turns out to be.
+size_t product_bytes(int dtype, int64_t M, int64_t N, int64_t K) {
+  int32_t splits = M ? plan_of(false, M, N, K).splits : 1;
+  if (M && dtype == EF_BF16) splits = std::max(splits, plan_of(true, M, N, K).splits);
+  return splits == 1 ? 0 : align_up((size_t)splits * ((size_t)M * padded(N) + (size_t)M) * 4, kAlign);
 }
 
 template <int KIND, int DT, int DO>
-int run_product(const Product& p, hipStream_t st) {
-  if constexpr (DT == EF_BF16) {
-    if (fast_ok<KIND>(p)) {
-      if (((p.M + 255) / 256) * ((p.N + 255) / 256) >= 192) return run_fast<KIND, DO, 256, 256, 2, 4>(p, st);
-      return run_fast<KIND, DO, 128, 128, 2, 2>(p, st);
+int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
+  const size_t need = product_bytes(DT, p.M, p.N, p.K);
+  if (need) {
+    if (!ws || !aligned(ws, kAlign)) return EF_EINVAL;
+    if (ws_bytes < need) return EF_EWORKSPACE;
+  }
+  const bool fast = DT == EF_BF16 && fast_ok<KIND>(p);
+  if constexpr (KIND == K_FWD && DT == EF_BF16) {
+    if (fast && p.M <= kFewTokens) {
+      // (32 outputs a workgroup where a group of the checkpoint needs them, or where half the workgroups fill the CUs)
+      const int ot = p.ep.k.codes || p.N >= 16 * 4 * kCUs ? 2 : 1;
+      const dim3 grid((unsigned)((p.N + 16 * ot - 1) / (16 * ot))), blk(kFewWaves * 64);
+#define EF_FEW(TT, OT) EF_LAUNCH((k_linear_few<TT, OT>), grid, blk, 0, st, (int32_t)p.M, (int32_t)p.N, (int32_t)p.K, p.A, p.B, p.ep)
+      if (p.M <= 16 && ot == 1) EF_FEW(1, 1);
+      else if (p.M <= 16) EF_FEW(1, 2);
+      else if (ot == 1) EF_FEW(2, 1);
+      else EF_FEW(2, 2);
+#undef EF_FEW
+      return launched();
     }
   }
-  const int64_t tiles = ((p.M + kAnyTile - 1) / kAnyTile) * ((p.N + kAnyTile - 1) / kAnyTile);
+  const Plan pl = plan_of(fast, p.M, p.N, p.K);
+  const Cost& c = kCosts[pl.form];
+  const int64_t tiles = ((p.M + c.tile - 1) / c.tile) * ((p.N + c.tile - 1) / c.tile);
   if (tiles > kMaxGrid) return EF_ERANGE;
-  EF_LAUNCH((k_linear_any<KIND, DT, DO>), dim3((unsigned)tiles), dim3(256), 0, st, (int32_t)p.M, (int32_t)p.N,
-            (int32_t)p.K, p.A, p.B, p.BK, p.ep);
+  Split sp{nullptr, nullptr, p.M * padded(p.N), padded(p.N), pl.per};
+  if (pl.splits > 1) {
+    sp.part = static_cast<float*>(ws);
+    sp.part_db = sp.part + (int64_t)pl.splits * sp.plane;
+  }
+  const dim3 grid((unsigned)tiles, (unsigned)pl.splits);
+  const int32_t M = (int32_t)p.M, N = (int32_t)p.N, K = (int32_t)p.K;
+  if constexpr (DT == EF_BF16) {
+    if (pl.form == kLarge) EF_LAUNCH((k_linear_bf16<KIND, DO, 256, 256, 2, 4>), grid, dim3(512), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
+    else if (pl.form == kSmall) EF_LAUNCH((k_linear_bf16<KIND, DO, 128, 128, 2, 2>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
+    else EF_LAUNCH((k_linear_any<KIND, DT, DO>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
+  } else {
+    EF_LAUNCH((k_linear_any<KIND, DT, DO>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
+  }
+  EF_TRY(launched());
+  if (pl.splits == 1) return EF_OK;
+  const int64_t lanes = p.M * (sp.Np / 8) + (KIND == K_WGRAD && p.ep.db ? p.M : 0);
+  EF_LAUNCH((k_linear_join<KIND, DO>), dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, st, M, N, (int)pl.splits, sp, p.ep);
   return launched();
 }
 
@@ -168,7 +248,8 @@ int ef_ckpt_act_backward(int64_t n, int64_t c, int act, const uint8_t* codes, co
 
 size_t ef_linear_workspace_bytes(int op, int64_t n, int64_t i, int64_t o, int dtype) {
   if (check_sizes(n, i, o) != EF_OK || !dtype_ok(dtype) || op < EF_OP_FORWARD || op > EF_OP_WGRAD) return 0;
-  return 0;
+  const int64_t M = op == EF_OP_WGRAD ? o : n, N = op == EF_OP_FORWARD ? o : i, K = op == EF_OP_FORWARD ? i : op == EF_OP_DGRAD ? o : n;
+  return product_bytes(dtype, M, N, K);
 }
 
 int ef_linear_forward(int64_t n, int64_t i, int64_t o, const void* x, int64_t ldx, const void* w, int64_t ldw,
@@ -188,9 +269,9 @@ int ef_linear_forward(int64_t n, int64_t i, int64_t o, const void* x, int64_t ld
   if (meet_any(out, rx, rw, rb, q, s) || meet_any(q, s, rx, rw, rb, rr) || meet_any(s, rx, rw, rb, rr)) return EF_EINVAL;
   if (meet(out, rr) && !(res == y && ldr == ldy)) return EF_EINVAL;
   if (n == 0) return EF_OK;
-  Product p{n, o, i, {x, ldx}, {w, ldw}, {}, {y, ldy, bias, res, ldr, {codes, scales, groups(o), fmt}, act, 0}};
-  return dtype == EF_F32 ? run_product<K_FWD, EF_F32, EF_F32>(p, S(stream))
-                         : run_product<K_FWD, EF_BF16, EF_BF16>(p, S(stream));
+  Product p{n, o, i, {x, ldx}, {w, ldw}, {}, {y, ldy, bias, res, ldr, {codes, scales, groups(o), fmt}, act, 0, nullptr}};
+  return dtype == EF_F32 ? run_product<K_FWD, EF_F32, EF_F32>(p, ws, ws_bytes, S(stream))
+                         : run_product<K_FWD, EF_BF16, EF_BF16>(p, ws, ws_bytes, S(stream));
 }
 
 int ef_linear_dgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t lddy, const void* w, int64_t ldw, int act,
@@ -209,9 +290,9 @@ int ef_linear_dgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t ldd
   if (meet(out, rr) && !(res == dx && ldr == lddx)) return EF_EINVAL;
   if (n == 0) return EF_OK;
   Product p{n, i, o, {dy, lddy}, {w, ldw}, {},
-            {dx, lddx, nullptr, res, ldr, {const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), groups(i), fmt}, act, 0}};
-  return dtype == EF_F32 ? run_product<K_DGRAD, EF_F32, EF_F32>(p, S(stream))
-                         : run_product<K_DGRAD, EF_BF16, EF_BF16>(p, S(stream));
+            {dx, lddx, nullptr, res, ldr, {const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), groups(i), fmt}, act, 0, nullptr}};
+  return dtype == EF_F32 ? run_product<K_DGRAD, EF_F32, EF_F32>(p, ws, ws_bytes, S(stream))
+                         : run_product<K_DGRAD, EF_BF16, EF_BF16>(p, ws, ws_bytes, S(stream));
 }
 
 int ef_linear_wgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t lddy, int dtype, const uint8_t* codes,
@@ -228,25 +309,12 @@ int ef_linear_wgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t ldd
   if (meet_any(rw, rb, ry, q, s) || meet_any(rb, ry, q, s)) return EF_EINVAL;
   hipStream_t st = S(stream);
   Product p{o, i, n, {dy, lddy}, {}, {const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), groups(i), fmt},
-            {dw, i, nullptr, nullptr, 0, {}, EF_ACT_NONE, accumulate ? 1 : 0}};
-  if (dtype == EF_F32) {
-    if (g_dtype == EF_F32) EF_TRY((run_product<K_WGRAD, EF_F32, EF_F32>(p, st)));
-    else EF_TRY((run_product<K_WGRAD, EF_F32, EF_BF16>(p, st)));
-  } else {
-    if (g_dtype == EF_F32) EF_TRY((run_product<K_WGRAD, EF_BF16, EF_F32>(p, st)));
-    else EF_TRY((run_product<K_WGRAD, EF_BF16, EF_BF16>(p, st)));
-  }
-  if (!db) return EF_OK;
-  const dim3 grid((unsigned)((o + 31) / 32)), blk(256);
-  const int add = accumulate ? 1 : 0;
-  if (dtype == EF_F32) {
-    if (g_dtype == EF_F32) EF_LAUNCH((k_bias_grad<EF_F32, EF_F32>), grid, blk, 0, st, n, (int32_t)o, dy, lddy, db, add);
-    else EF_LAUNCH((k_bias_grad<EF_F32, EF_BF16>), grid, blk, 0, st, n, (int32_t)o, dy, lddy, db, add);
-  } else {
-    if (g_dtype == EF_F32) EF_LAUNCH((k_bias_grad<EF_BF16, EF_F32>), grid, blk, 0, st, n, (int32_t)o, dy, lddy, db, add);
-    else EF_LAUNCH((k_bias_grad<EF_BF16, EF_BF16>), grid, blk, 0, st, n, (int32_t)o, dy, lddy, db, add);
-  }
-  return launched();
+            {dw, i, nullptr, nullptr, 0, {}, EF_ACT_NONE, accumulate ? 1 : 0, db}};
+  if (dtype == EF_F32)
+    return g_dtype == EF_F32 ? run_product<K_WGRAD, EF_F32, EF_F32>(p, ws, ws_bytes, st)
+                             : run_product<K_WGRAD, EF_F32, EF_BF16>(p, ws, ws_bytes, st);
+  return g_dtype == EF_F32 ? run_product<K_WGRAD, EF_BF16, EF_F32>(p, ws, ws_bytes, st)
+                           : run_product<K_WGRAD, EF_BF16, EF_BF16>(p, ws, ws_bytes, st);
 }
 
 }  // extern "C"

@@ -329,24 +329,70 @@ struct Epi {
   void* db;           // wgrad: [M], the sums of A's lines, or null
 };
 
-// KIND the product, DT the type of out, bias and res.
+// What the epilogue reads beside C for eight columns of a row, loaded ahead of its use; KIND the product, DT the type
+// of out, bias and res.
 template <int KIND, int DT>
-__device__ __forceinline__ void epilogue8(const Epi& a, int64_t row, int32_t col, bool row_ok, int32_t N,
-                                          float (&v)[8]) {
-  const int cnt = row_ok ? N - col : 0;  // columns of this lane that exist (8 or more: all)
-  if (KIND == K_FWD) {
-    if (a.bias) {
-      float b[8];
-      load8<DT>(a.bias, col, N - col, b);
+struct Side {
+  static constexpr int W = DT == EF_F32 ? 8 : 4;
+  uint32_t r[W];  // res, or the old dw, as stored
+  u32x2 q;        // dgrad: the kept codes and their scale
+  uint32_t s;
+
+  __device__ __forceinline__ void raw(const void* p, int64_t at, int cnt) {
+    if (cnt >= 8) {
+      const u32x4u* from = reinterpret_cast<const u32x4u*>(static_cast<const char*>(p) + at * (W / 2));
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += b[j];
+      for (int j = 0; j < W / 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[4 * j + i] = from[j][i];
+    } else {
+      float v[8];
+      load8<DT>(p, at, cnt, v);
+#pragma unroll
+      for (int j = 0; j < W; ++j) r[j] = DT == EF_F32 ? __float_as_uint(v[j]) : f_bf16x2(v[2 * j % 8], v[(2 * j + 1) % 8]);
     }
-    if (a.k.codes) {  // (every lane of a group takes part)
+  }
+  __device__ __forceinline__ float value(int j) const {
+    if (DT == EF_F32) return __uint_as_float(r[j % W]);
+    return __uint_as_float(j & 1 ? r[j / 2 % W] & 0xFFFF0000u : r[j / 2 % W] << 16);
+  }
+
+  // cnt of the eight columns exist (8 or more: all; 0 or less: none)
+  __device__ __forceinline__ void load(const Epi& a, int64_t row, int32_t col, int cnt) {
+    if (cnt <= 0) return;
+    if (KIND == K_DGRAD && a.act != EF_ACT_NONE) {
+      q = *reinterpret_cast<const u32x2*>(a.k.codes + row * a.k.G * kGroup + col);
+      s = a.k.scales[row * a.k.G + col / kGroup];
+    }
+    if (KIND == K_WGRAD) {
+      if (a.add) raw(a.out, row * a.ldo + col, cnt);
+    } else if (a.res) {
+      raw(a.res, row * a.ldr + col, cnt);
+    }
+  }
+};
+
+template <int KIND, int DT>
+__device__ __forceinline__ void load_bias(const Epi& a, int32_t col, int32_t N, float (&b)[8]) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = j < cnt ? v[j] : 0.0f;
+  for (int j = 0; j < 8; ++j) b[j] = 0.0f;
+  if (KIND == K_FWD && a.bias) load8<DT>(a.bias, col, N - col, b);
+}
+
+// Four neighbouring lanes hold a group of 32 columns and call this together.
+template <int KIND, int DT>
+__device__ __forceinline__ void epilogue8(const Epi& a, int64_t row, int32_t col, int cnt, float (&v)[8], const float (&b)[8],
+                                          const Side<KIND, DT>& side) {
+  if (KIND == K_FWD) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += b[j];
+    if (a.k.codes) {
+      if (cnt < 8)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < cnt ? v[j] : 0.0f;
       const uint32_t s = group_scale(group_amax(v), a.k.fmt);
-      if (row_ok && col < a.k.G * kGroup) {
-        *reinterpret_cast<u32x2u*>(a.k.codes + row * a.k.G * kGroup + col) = encode8(v, s, a.k.fmt);
+      if (cnt > -kGroup && col < a.k.G * kGroup) {  // (the group's columns behind the last one: code 0)
+        *reinterpret_cast<u32x2*>(a.k.codes + row * a.k.G * kGroup + col) = encode8(v, s, a.k.fmt);
         if ((col & (kGroup - 1)) == 0) a.k.scales[row * a.k.G + col / kGroup] = (uint8_t)s;
       }
     }
@@ -355,24 +401,18 @@ __device__ __forceinline__ void epilogue8(const Epi& a, int64_t row, int32_t col
   if (cnt <= 0) return;
   if (KIND == K_DGRAD && a.act != EF_ACT_NONE) {
     float z[8];
-    decode8(*reinterpret_cast<const u32x2u*>(a.k.codes + row * a.k.G * kGroup + col),
-            a.k.scales[row * a.k.G + col / kGroup], a.k.fmt, z);
+    decode8(side.q, side.s, a.k.fmt, z);
     act_slope(v, z, a.act);
   }
-  if (KIND != K_WGRAD && a.res) {
-    float r[8];
-    load8<DT>(a.res, row * a.ldr + col, cnt, r);
+  if (KIND == K_WGRAD ? a.add != 0 : a.res != nullptr) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += r[j];
-  }
-  if (KIND == K_WGRAD && a.add) {
-    float r[8];
-    load8<DT>(a.out, row * a.ldo + col, cnt, r);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = r[j] + v[j];
+    for (int j = 0; j < 8; ++j) v[j] = side.value(j) + v[j];
   }
   store8<DT>(a.out, row * a.ldo + col, cnt, v);
 }
+
+// No column of this row: less than any distance to the last column's group.
+constexpr int kNoRow = -0x40000000;
 
 template <int DO>
 __device__ __forceinline__ void store_db(const Epi& a, int64_t m, float s) {
@@ -394,37 +434,55 @@ struct Split {
   int32_t per;     // steps per split
 };
 
-// A wavefront's 32 x 64 of C, handed over through its part of the LDS: from lanes that hold single columns (four
-// rows each) to lanes that hold eight columns of a row.  Every wavefront of the workgroup takes part.
+// A wavefront's T times 32 x 64 of C, handed over 32 rows at a time through its own part of the LDS (a wavefront's
+// reads and writes of the LDS keep their order): from lanes that hold single columns, four rows each, to lanes that
+// hold eight columns of a row.  What the epilogue reads beside C is loaded 32 rows ahead.
 constexpr int kSlabPitch = 68;
-template <int KIND, int DO>
-__device__ __forceinline__ void finish(const f32x16 (&acc)[2], float* slab, int lane, int64_t row0, int64_t col0, int32_t M,
+template <int KIND, int DO, int T>
+__device__ __forceinline__ void finish(const f32x16 (&acc)[T][2], float* slab, int lane, int64_t row0, int64_t col0, int32_t M,
                                        int32_t N, const Epi& ep, const Split& sp) {
+  const int rr = lane >> 3;
+  const int32_t col = (int32_t)col0 + (lane & 7) * 8;
+  float bias[8];
+  Side<KIND, DO> side[2][4];
+  auto ahead = [&](int a) {
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      slab[((r >> 2) * 8 + (lane >> 5) * 4 + (r & 3)) * kSlabPitch + b * 32 + (lane & 31)] = acc[b][r];
-  __syncthreads();
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int rr = q * 8 + (lane >> 3), cc = (lane & 7) * 8;
-    const f32x4 lo = *reinterpret_cast<const f32x4*>(slab + rr * kSlabPitch + cc);
-    const f32x4 hi = *reinterpret_cast<const f32x4*>(slab + rr * kSlabPitch + cc + 4);
-    const int64_t row = row0 + rr;
-    const int32_t col = (int32_t)(col0 + cc);
-    if (sp.part) {
-      if (row < M && col < sp.Np) {
-        float* p = sp.part + blockIdx.y * sp.plane + row * sp.Np + col;
-        *reinterpret_cast<f32x4*>(p) = lo;
-        *reinterpret_cast<f32x4*>(p + 4) = hi;
-      }
-    } else {
-      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      epilogue8<KIND, DO>(ep, row, col, row < M, N, v);
+    for (int q = 0; q < 4; ++q) {
+      const int64_t row = row0 + a * 32 + q * 8 + rr;
+      side[a & 1][q].load(ep, row, col, row < M ? N - col : kNoRow);
     }
+  };
+  if (!sp.part) {
+    load_bias<KIND, DO>(ep, col, N, bias);
+    ahead(0);
   }
-  __syncthreads();
+#pragma unroll
+  for (int a = 0; a < T; ++a) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        slab[((r >> 2) * 8 + (lane >> 5) * 4 + (r & 3)) * kSlabPitch + b * 32 + (lane & 31)] = acc[a][b][r];
+    asm volatile("" ::: "memory");
+    if (!sp.part && a + 1 < T) ahead(a + 1);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t row = row0 + a * 32 + q * 8 + rr;
+      const float* from = slab + (q * 8 + rr) * kSlabPitch + (lane & 7) * 8;
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(from), hi = *reinterpret_cast<const f32x4*>(from + 4);
+      if (sp.part) {
+        if (row < M && col < sp.Np) {
+          float* p = sp.part + blockIdx.y * sp.plane + row * sp.Np + col;
+          *reinterpret_cast<f32x4*>(p) = lo;
+          *reinterpret_cast<f32x4*>(p + 4) = hi;
+        }
+      } else {
+        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        epilogue8<KIND, DO>(ep, row, col, row < M ? N - col : kNoRow, v, bias, side[a & 1][q]);
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
 }
 
 // wgrad, the wavefronts of the first column of tiles: the sums of A's lines that went by; two lanes hold a line.
@@ -536,8 +594,7 @@ __global__ __launch_bounds__(256) void k_linear_any(int32_t M, int32_t N, int32_
   }
   __syncthreads();
   float* slab = sm + wave * 32 * kSlabPitch;
-#pragma unroll
-  for (int a = 0; a < 2; ++a) finish<KIND, DO>(acc[a], slab, lane, m0 + wm + a * 32, n0 + wn, M, N, ep, sp);
+  finish<KIND, DO, 2>(acc, slab, lane, m0 + wm, n0 + wn, M, N, ep, sp);
   if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
 }
 
@@ -570,22 +627,30 @@ constexpr int64_t kFastLd = (int64_t)1 << 21;  // leading dimensions up to this 
 // (the host pass does not know the buffer type)
 #if defined(__HIP_DEVICE_COMPILE__)
 #define EF_BUFFER(P, BYTES) __builtin_amdgcn_make_buffer_rsrc((void*)(P), 0, (int)(BYTES), 0x00020000)
-#define EF_BUFFER_TO_LDS(R, LDS, OFF) __builtin_amdgcn_raw_ptr_buffer_load_lds(R, (EF_LDS void*)(LDS), 16, OFF, 0, 0, 0)
 #define EF_BUFFER_B128(R, OFF) __builtin_amdgcn_raw_buffer_load_b128(R, OFF, 0, 0)
-#define EF_BUFFER_B64(R, OFF) __builtin_amdgcn_raw_buffer_load_b64(R, OFF, 0, 0)
 #define EF_BUFFER_B8(R, OFF) __builtin_amdgcn_raw_buffer_load_b8(R, OFF, 0, 0)
 #else
 #define EF_BUFFER(P, BYTES) (BYTES)
-#define EF_BUFFER_TO_LDS(R, LDS, OFF) ((void)(R), (void)(OFF))
 #define EF_BUFFER_B128(R, OFF) (u32x4{(uint32_t)(R), (uint32_t)(OFF), 0u, 0u})
-#define EF_BUFFER_B64(R, OFF) (u32x2{(uint32_t)(R), 0u})
 #define EF_BUFFER_B8(R, OFF) ((uint32_t)(R))
 #endif
+
+// 16 bytes a lane from offset `off` of a buffer to the LDS, the lanes side by side from lds on; what lies outside the
+// buffer arrives as zeros.  Written out: the compiler, which cannot tell the two halves of the LDS apart, would let
+// later reads of the LDS wait for it.  It has no result register; the wait before the barrier covers it.
+__device__ __forceinline__ void buffer_to_lds(const char* base, uint32_t bytes, const char* lds, int off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint64_t b = reinterpret_cast<uint64_t>(base);
+  const u32x4 r = {(uint32_t)b, (uint32_t)(b >> 32), bytes, 0x00020000u};
+  const uint32_t at = (uint32_t)reinterpret_cast<uintptr_t>((EF_LDS const char*)lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(r) : "memory");
+#endif
+}
 
 // One operand's way into the LDS.  KC: k along the row.  LINES rows of C (or columns) per tile, NW wavefronts.
 template <bool KC, int LINES, int NW>
 struct Stream {
-  static constexpr int J = LINES * kBK * 2 / 1024 / NW;  // 1024 bytes per wavefront and load
+  static constexpr int J = LINES * kBK * 2 / 1024 / NW;  // loads per wavefront and step, 1024 bytes each
   static_assert(NW % 2 == 0, "a wavefront's loads are all of even or all of odd eights of lines");
   const char* base;
   int64_t step;   // bytes from one step to the next
@@ -620,77 +685,87 @@ struct Stream {
     }
   }
 
-  // the tile of step s into lds (LINES * 128 bytes)
-  __device__ __forceinline__ void load(int64_t s, char* lds, int wave) const {
+  // part j of the tile of step s into lds (LINES * 128 bytes in all)
+  __device__ __forceinline__ void load(int j, int64_t s, char* lds, int wave) const {
     const int64_t kleft = K - s * kBK;
-    const int64_t limit = KC ? left - s * step : ((kleft < kBK ? kleft : kBK) - 1) * ld2 + left;
-    const auto r = EF_BUFFER(base + s * step, limit);
-    const bool in = !KC || chunk8 < kleft;
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-      EF_BUFFER_TO_LDS(r, lds + (j * NW + wave) * 1024, in ? off[j] : kFar);
+    int64_t limit = KC ? left - s * step : ((kleft < kBK ? kleft : kBK) - 1) * ld2 + left;
+    if (kleft <= 0) limit = 0;  // (behind the last step: zeros, which nothing reads)
+    buffer_to_lds(base + s * step, (uint32_t)limit, lds + (j * NW + wave) * 1024, !KC || chunk8 < kleft ? off[j] : kFar);
   }
 };
 
-// A checkpoint's way: NT threads, LINES columns per tile; eight codes a chunk.
-template <int LINES, int NT>
+// A checkpoint's way: NT threads, LINES columns per tile; a thread has J chunks of sixteen codes, half a group each,
+// in registers, and passes them on as bfloat16 in quarters of a step.
+template <int FMT, int LINES, int NT>
 struct StreamKept {
-  static constexpr int J = kBK * LINES / 8 / NT;
+  static constexpr int J = kBK * LINES / 16 / NT;
+  static_assert(J == 2, "four times eight codes");
+  struct Codes {
+    u32x4 q[J];
+    uint32_t s[J];
+  };
   const uint8_t *codes, *scales;
   int64_t K;
-  int32_t row_bytes, G, fmt, left;
+  int32_t row_bytes, G, left;
   int off[J], soff[J], to[J];
-  u32x2 q[J];
-  uint32_t s[J];
 
   __device__ __forceinline__ void init(const Kept& k, int64_t line0, int64_t rows, int tid) {
     row_bytes = k.G * kGroup;
     G = k.G;
-    fmt = k.fmt;
     K = rows;
     codes = k.codes + line0;
     scales = k.scales + line0 / kGroup;
     left = row_bytes - (int32_t)line0;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const int id = j * NT + tid, row = id / (LINES / 8), c = id % (LINES / 8);
-      const bool in = c * 8 < left;
-      off[j] = in ? row * row_bytes + c * 8 : kFar;
-      soff[j] = in ? row * G + c / 4 : kFar;
-      to[j] = row * LINES * 2 + (((c >> 2) ^ (row & 3)) << 6) + (c & 3) * 16;
+      const int id = j * NT + tid, row = id / (LINES / 16), c = id % (LINES / 16);
+      const bool in = c * 16 < left;
+      off[j] = in ? row * row_bytes + c * 16 : kFar;
+      soff[j] = in ? row * G + c / 2 : kFar;
+      to[j] = row * LINES * 2 + (((c >> 1) ^ (row & 3)) << 6) + (c & 1) * 32;
     }
   }
-  __device__ __forceinline__ void fetch(int64_t step) {
-    const int64_t k0 = step * kBK;
-    const int rows = K - k0 < kBK ? (int)(K - k0) : kBK;
-    const auto rc = EF_BUFFER(codes + k0 * row_bytes, (rows - 1) * row_bytes + left);
-    const auto rs = EF_BUFFER(scales + k0 * G, (rows - 1) * G + left / kGroup);
+  // the codes of a step (outside the matrix: zeros, as the scales, and 0 * 0 is what they decode to)
+  __device__ __forceinline__ void fetch(int64_t step, Codes& c) const {
+    const int64_t k0 = step * kBK, kleft = K - k0;
+    const int rows = kleft < kBK ? (int)kleft : kBK;
+    const auto rc = EF_BUFFER(codes + k0 * row_bytes, kleft > 0 ? (rows - 1) * row_bytes + left : 0);
+    const auto rs = EF_BUFFER(scales + k0 * G, kleft > 0 ? (rows - 1) * G + left / kGroup : 0);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      q[j] = EF_BUFFER_B64(rc, off[j]);
-      s[j] = EF_BUFFER_B8(rs, soff[j]);
+      c.q[j] = EF_BUFFER_B128(rc, off[j]);
+      c.s[j] = EF_BUFFER_B8(rs, soff[j]);
     }
   }
-  __device__ __forceinline__ void store(char* lds) const {
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      u32x4 w;
-      if (fmt == EF_CKPT_INT8) {
-        float v[8];
-        decode8(q[j], s[j], EF_CKPT_INT8, v);
-#pragma unroll
-        for (int h = 0; h < 4; ++h)  // (exact: the low halves are zeros)
-          w[h] = __builtin_amdgcn_perm(__float_as_uint(v[2 * h + 1]), __float_as_uint(v[2 * h]), 0x07060302u);
-      } else {
-        const float r = __uint_as_float(s[j] << 23);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          w[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[j][h], r, false));
-          w[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[j][h], r, true));
-        }
-      }
-      *reinterpret_cast<u32x4*>(lds + to[j]) = w;
+  // the signed byte 2 * HI or 2 * HI + 1 of w as a float (written out: the compiler, given the conversion, keeps the
+  // bytes of a whole step apart and spills)
+  template <int HI>
+  static __device__ __forceinline__ void bytes(uint32_t w, float* a, float* b) {
+    if (HI) {
+      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(*a) : "v"(w));
+      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(*b) : "v"(w));
+    } else {
+      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(*a) : "v"(w));
+      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(*b) : "v"(w));
     }
+  }
+  // codes 2 h and 2 h + 1 of quarter f
+  __device__ __forceinline__ uint32_t pair(const Codes& c, int f, int h) const {
+    const uint32_t w = c.q[f >> 1][(f & 1) * 2 + (h >> 1)];
+    const float r = __uint_as_float(c.s[f >> 1] << 23);
+    if (FMT == EF_CKPT_INT8) {
+      float a, b;
+      if (h & 1) bytes<1>(w, &a, &b);
+      else bytes<0>(w, &a, &b);
+      a *= r;
+      b *= r;
+      return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);  // (exact: the low halves are zeros)
+    }
+    return __builtin_bit_cast(uint32_t, h & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, r, true)
+                                              : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, r, false));
+  }
+  __device__ __forceinline__ void put(int f, u32x4 w, char* lds) const {
+    *reinterpret_cast<u32x4*>(lds + to[f >> 1] + (f & 1) * 16) = w;
   }
 };
 
@@ -710,18 +785,12 @@ struct Reader {
         off[t] = ((lane >> 5) * 8 + x) * LINES * 2 + (((line0 / 32 + t) ^ x) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
     }
   }
-  __device__ __forceinline__ void read(const char* lds, int ks, bf16x8 (&f)[T]) const {
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-      if (KC) {
-        f[t] = *reinterpret_cast<const bf16x8*>(lds + off[ks] + t * 32 * 128);
-      } else {
-        const char* p = lds + off[t] + ks * 16 * LINES * 2;
-        const bf16x4 a = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((EF_LDS s16x4*)p));
-        const bf16x4 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((EF_LDS s16x4*)(p + 4 * LINES * 2)));
-        f[t] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-    }
+  __device__ __forceinline__ bf16x8 read(const char* lds, int ks, int t) const {
+    if (KC) return *reinterpret_cast<const bf16x8*>(lds + off[ks] + t * 32 * 128);
+    const char* p = lds + off[t] + ks * 16 * LINES * 2;
+    const bf16x4 a = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((EF_LDS s16x4*)p));
+    const bf16x4 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((EF_LDS s16x4*)(p + 4 * LINES * 2)));
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 };
 
@@ -743,7 +812,7 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tm, uint32_t tn, ui
   *n = in / h;
 }
 
-template <int KIND, int DO, int BM, int BN, int WM, int WN>
+template <int KIND, int DO, int FMT, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32_t N, int32_t K, Mat A, Mat B, Kept BK, Epi ep, Split sp) {
   constexpr bool AKC = KIND != K_WGRAD, BKC = KIND == K_FWD, B8 = KIND == K_WGRAD;
   constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
@@ -761,7 +830,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
   Stream<AKC, BM, NW> sa;
   sa.init(A, m0, M, K, wave, lane);
   Stream<BKC, BN, NW> sb;
-  StreamKept<BN, NW * 64> sk;
+  using SK = StreamKept<FMT, BN, NW * 64>;
+  SK sk;
   if (B8) sk.init(BK, n0, K, tid);
   else sb.init(B, n0, N, K, wave, lane);
   Reader<AKC, BM, TM> ra;
@@ -781,74 +851,117 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
 #pragma unroll
   for (int a = 0; a < TM; ++a) bs[a] = 0.0f;
   bf16x8 fa[2][TM], fb[2][TN];
-  auto mul = [&](int h) {
+  // One slice: the matrix instructions of the fragments h, and between them, one by one, the reads of the next ones
+  // (slice ks of rd) and whatever else there is to do.  Pinned in this order: left to itself the compiler gathers the
+  // reads before their use.
+  constexpr int kMul = TM * TN;
+  auto slice = [&](int h, const char* rd, int ks, auto&& between) {
 #pragma unroll
-    for (int a = 0; a < TM; ++a)
+    for (int i = 0; i < kMul; ++i) {
+      const int a = i / TN, b = i % TN;
+      acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[h][a], fb[h][b], acc[a][b], 0, 0, 0);
+      if (rd) {
+        if (i < TN) fb[h ^ 1][i] = rb.read(rd + kA, ks, i);
+        else if (i - TN < TM) fa[h ^ 1][i - TN] = ra.read(rd, ks, i - TN);
+        if (i == kMul - 1)
 #pragma unroll
-      for (int b = 0; b < TN; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[h][a], fb[h][b], acc[a][b], 0, 0, 0);
+          for (int t = kMul - TN; t < TM; ++t) fa[h ^ 1][t] = ra.read(rd, ks, t);
+      }
+      between(i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     if (sums) {
 #pragma unroll
       for (int a = 0; a < TM; ++a) bs[a] = add8(fa[h][a], bs[a]);
     }
   };
-
-  sa.load(s0, lds, wave);
-  if (B8) {
-    sk.fetch(s0);
-    sk.store(lds + kA);
-  } else {
-    sb.load(s0, lds + kA, wave);
-  }
-  if (s0 + 1 < s1) {
-    sa.load(s0 + 1, lds + kHalf, wave);
-    if (B8) {
-      sk.fetch(s0 + 1);
-      sk.store(lds + kHalf + kA);
-      if (s0 + 2 < s1) sk.fetch(s0 + 2);
-    } else {
-      sb.load(s0 + 1, lds + kHalf + kA, wave);
+  // Step s + 2 goes into the half of step s from the barrier on that ends step s; the instructions of its last
+  // fragments (slice 3) come behind that barrier.  A checkpoint's codes arrive in registers by the same barrier as
+  // the other operand of the step before, and follow it a quarter a slice.
+  using SA = Stream<AKC, BM, NW>;
+  using SB = Stream<BKC, BN, NW>;
+  typename SK::Codes codes[2];
+  u32x4 w;
+  auto quarter = [&](int i, const typename SK::Codes& c, int f, char* to) {
+    constexpr int P = 4 / (kMul / 2);
+    if (i < kMul / 2) {
+#pragma unroll
+      for (int h = 0; h < P; ++h) w[i * P + h] = sk.pair(c, f, i * P + h);
     }
+    if (i == kMul / 2) sk.put(f, w, to + kA);
+  };
+  auto tile = [&](int64_t s, char* to) {
+#pragma unroll
+    for (int j = 0; j < SA::J; ++j) sa.load(j, s, to, wave);
+    if (!B8)
+#pragma unroll
+      for (int j = 0; j < SB::J; ++j) sb.load(j, s, to + kA, wave);
+  };
+  auto decode = [&](const typename SK::Codes& c, int f0, int f1, char* to) {
+#pragma unroll
+    for (int f = f0; f < f1; ++f) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) w[h] = sk.pair(c, f, h);
+      sk.put(f, w, to + kA);
+    }
+  };
+  char* const half0 = lds;
+  char* const half1 = lds + kHalf;
+  if (B8) {
+    sk.fetch(s0, codes[0]);
+    sk.fetch(s0 + 1, codes[1]);
+  }
+  tile(s0, half0);
+  tile(s0 + 1, half1);
+  if (B8) {
+    decode(codes[0], 0, 4, half0);
+    decode(codes[1], 0, 1, half1);
+    sk.fetch(s0 + 2, codes[0]);
   }
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
-  ra.read(lds, 0, fa[0]);
-  rb.read(lds + kA, 0, fb[0]);
-  char* cur = lds;
-  char* nxt = lds + kHalf;
-  auto slices = [&]() {
 #pragma unroll
-    for (int ks = 0; ks < 3; ++ks) {
-      ra.read(cur, ks + 1, fa[(ks + 1) & 1]);
-      rb.read(cur + kA, ks + 1, fb[(ks + 1) & 1]);
-      mul(ks & 1);
-    }
-  };
-  for (int64_t s = s0; s + 1 < s1; ++s) {
-    slices();
-    __builtin_amdgcn_s_waitcnt(0);  // this wavefront's part of the next step has arrived, its last reads are done
-    __syncthreads();
-    if (s + 2 < s1) {
-      sa.load(s + 2, cur, wave);
-      if (B8) {
-        sk.store(cur + kA);
-        if (s + 3 < s1) sk.fetch(s + 3);
-      } else {
-        sb.load(s + 2, cur + kA, wave);
+  for (int t = 0; t < TM; ++t) fa[0][t] = ra.read(half0, 0, t);
+#pragma unroll
+  for (int t = 0; t < TN; ++t) fb[0][t] = rb.read(half0 + kA, 0, t);
+  // Step s in cur, s + 1 in nxt (of its checkpoint, in `now`, a quarter); `then` has the codes of s + 2.
+  auto advance = [&](int64_t s, char* cur, char* nxt, typename SK::Codes& now, typename SK::Codes& then) {
+#pragma unroll
+    for (int ks = 0; ks < 3; ++ks)
+      slice(ks & 1, cur, ks + 1, [&](int i) {
+        if (B8) quarter(i, now, ks + 1, nxt);
+      });
+    // This wavefront's part of the next step has arrived, and its last reads of this one.
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    slice(1, nxt, 0, [&](int i) {
+      if (B8 && i == 0) sk.fetch(s + 3, now);
+      constexpr int D = B8 ? SA::J : SA::J + SB::J, Q = (D + kMul - 1) / kMul;
+#pragma unroll
+      for (int d = 0; d < Q; ++d) {
+        const int j = i * Q + d;
+        if (j < SA::J) sa.load(j, s + 2, cur, wave);
+        else if (!B8 && j < D) sb.load(j - SA::J, s + 2, cur + kA, wave);
       }
-    }
-    ra.read(nxt, 0, fa[0]);
-    rb.read(nxt + kA, 0, fb[0]);
-    mul(1);
-    char* x = cur;
-    cur = nxt;
-    nxt = x;
+      if (B8) quarter(i, then, 0, cur);
+    });
+  };
+  int64_t s = s0;
+  for (; s + 2 < s1; s += 2) {
+    advance(s, half0, half1, codes[1], codes[0]);
+    advance(s + 1, half1, half0, codes[0], codes[1]);
   }
-  slices();
-  mul(1);
+  const char* last = half0;
+  if (s + 1 < s1) {
+    advance(s, half0, half1, codes[1], codes[0]);
+    last = half1;
+  }
+#pragma unroll
+  for (int ks = 0; ks < 3; ++ks) slice(ks & 1, last, ks + 1, [](int) {});
+  slice(1, nullptr, 0, [](int) {});
+  __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   float* slab = reinterpret_cast<float*>(lds) + wave * 32 * kSlabPitch;
-#pragma unroll
-  for (int a = 0; a < TM; ++a) finish<KIND, DO>(acc[a], slab, lane, m0 + wm + a * 32, n0 + wn, M, N, ep, sp);
+  finish<KIND, DO, TM>(acc, slab, lane, m0 + wm, n0 + wn, M, N, ep, sp);
   if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
 }
 
@@ -907,6 +1020,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_linear_few(int32_t n, int32_
   // eight outputs of a token per lane; four neighbouring lanes a group where OT is 2
   if (tid >= TT * 16 * OT * 2) return;
   const int q = tid % (OT * 2), token = tid / (OT * 2);
+  const int32_t col = (int32_t)o0 + q * 8;
+  const int cnt = token < n ? N - col : kNoRow;
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
   for (int z = 0; z < kFewWaves; ++z) {
@@ -918,7 +1033,11 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_linear_few(int32_t n, int32_
       v[j + 4] += hi[j];
     }
   }
-  epilogue8<K_FWD, EF_BF16>(ep, token, (int32_t)o0 + q * 8, token < n, N, v);
+  float b[8];
+  Side<K_FWD, EF_BF16> side;
+  load_bias<K_FWD, EF_BF16>(ep, col, N, b);
+  side.load(ep, token, col, cnt);
+  epilogue8<K_FWD, EF_BF16>(ep, token, col, cnt, v, b, side);
 }
 
 // The splits' sums in order, then the epilogue.  Np / 8 lanes a row, whole groups side by side.
@@ -937,7 +1056,11 @@ __global__ __launch_bounds__(256) void k_linear_join(int32_t M, int32_t N, int s
     store_db<DO>(ep, m, t);
     return;
   }
-  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  const int cnt = in ? N - col : kNoRow;
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, b[8];
+  Side<KIND, DO> side;
+  load_bias<KIND, DO>(ep, col, N, b);
+  side.load(ep, row, col, cnt);
   if (in)
     for (int z = 0; z < splits; ++z) {
       const float* p = sp.part + z * sp.plane + row * sp.Np + col;
@@ -948,7 +1071,7 @@ __global__ __launch_bounds__(256) void k_linear_join(int32_t M, int32_t N, int s
         v[j + 4] += hi[j];
       }
     }
-  epilogue8<KIND, DO>(ep, row, col, in, N, v);
+  epilogue8<KIND, DO>(ep, row, col, cnt, v, b, side);
 }
 
 }  // namespace efs

@@ -176,13 +176,26 @@ int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
   }
   const dim3 grid((unsigned)tiles, (unsigned)pl.splits);
   const int32_t M = (int32_t)p.M, N = (int32_t)p.N, K = (int32_t)p.K;
+#define EF_FORM(FMT)                                                                                                  \
+  do {                                                                                                                \
+    if (pl.form == kLarge)                                                                                            \
+      EF_LAUNCH((k_linear_bf16<KIND, DO, FMT, 256, 256, 2, 4>), grid, dim3(512), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp); \
+    else                                                                                                              \
+      EF_LAUNCH((k_linear_bf16<KIND, DO, FMT, 128, 128, 2, 2>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp); \
+  } while (0)
   if constexpr (DT == EF_BF16) {
-    if (pl.form == kLarge) EF_LAUNCH((k_linear_bf16<KIND, DO, 256, 256, 2, 4>), grid, dim3(512), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
-    else if (pl.form == kSmall) EF_LAUNCH((k_linear_bf16<KIND, DO, 128, 128, 2, 2>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
-    else EF_LAUNCH((k_linear_any<KIND, DT, DO>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
+    if (pl.form == kAny) {
+      EF_LAUNCH((k_linear_any<KIND, DT, DO>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
+    } else if constexpr (KIND == K_WGRAD) {
+      if (p.BK.fmt == EF_CKPT_E4M3) EF_FORM(EF_CKPT_E4M3);
+      else EF_FORM(EF_CKPT_INT8);
+    } else {
+      EF_FORM(EF_CKPT_INT8);  // (read no checkpoint along k)
+    }
   } else {
     EF_LAUNCH((k_linear_any<KIND, DT, DO>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
   }
+#undef EF_FORM
   EF_TRY(launched());
   if (pl.splits == 1) return EF_OK;
   const int64_t lanes = p.M * (sp.Np / 8) + (KIND == K_WGRAD && p.ep.db ? p.M : 0);

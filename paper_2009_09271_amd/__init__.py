@@ -505,59 +505,75 @@ def ef_step_randblock(layout, g, e, seed, step, start, val, stream=None):
 # Matrices are two-dimensional tensors whose rows are contiguous (any row stride of at least a row); all of a call's
 # tensors are on one GPU, whose current stream (or `stream`) the call is enqueued on.
 
-def _arg(t, name, where, dtypes, rows=None, cols=None, dev=None):
-    """Checks a matrix argument (a vector where rows is 0) before its pointer crosses the ABI."""
+def _refuse(t, name, where, dtypes, dev, n, c):
+    """Says why a matrix argument (a vector of c where n is -1) does not fit."""
     import torch
     if not isinstance(t, torch.Tensor):
-        raise EfError(EF_EINVAL, where, f"{name} is None" if t is None else f"{name} is not a tensor")
-    if not t.is_cuda:
-        raise EfError(EF_EINVAL, where, f"{name} is not on a GPU")
-    if dev is not None and t.device != dev:
-        raise EfError(EF_EINVAL, where, f"{name} is on {t.device}, not on {dev}")
-    if t.dtype not in dtypes:
-        raise EfError(EF_EINVAL, where, f"{name} has dtype {t.dtype}")
-    if rows == 0:
-        if t.dim() != 1 or t.shape[0] != cols or (cols > 1 and t.stride(0) != 1):
-            raise EfError(EF_EINVAL, where, f"{name} is not a contiguous vector of {cols}")
-        return t
-    if t.dim() != 2:
-        raise EfError(EF_EINVAL, where, f"{name} is not a matrix")
-    n, c = t.shape
-    if (rows is not None and n != rows[0]) or (cols is not None and c != cols):
-        raise EfError(EF_EINVAL, where, f"{name} has shape {tuple(t.shape)}, "
-                                        f"{(rows[0] if rows is not None else n, cols if cols is not None else c)} needed")
-    if c > 1 and t.stride(1) != 1 or n > 1 and t.stride(0) < c:
-        raise EfError(EF_EINVAL, where, f"{name} has strides {tuple(t.stride())}: its rows must be contiguous and apart")
-    return t
+        why = f"{name} is None" if t is None else f"{name} is not a tensor"
+    elif not t.is_cuda:
+        why = f"{name} is not on a GPU"
+    elif dev is not None and t.device != dev:
+        why = f"{name} is on {t.device}, not on {dev}"
+    elif t.dtype not in dtypes:
+        why = f"{name} has dtype {t.dtype}"
+    elif n == -1:
+        why = f"{name} is not a contiguous vector of {c}"
+    elif t.dim() != 2:
+        why = f"{name} is not a matrix"
+    elif (n is not None and t.shape[0] != n) or (c is not None and t.shape[1] != c):
+        why = f"{name} has shape {tuple(t.shape)}, {(t.shape[0] if n is None else n, t.shape[1] if c is None else c)} needed"
+    else:
+        why = f"{name} has strides {t.stride()}: its rows must be contiguous and apart"
+    raise EfError(EF_EINVAL, where, why)
 
 
-def _ld(t):
-    """Elements from one row to the next (a single row's own length, whatever its stride says)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _mat(t, name, where, dtypes, dev=None, n=None, c=None):
+    """Checks a matrix argument before its pointer crosses the ABI; its elements from one row to the next (a single
+    row's own length, whatever its stride says)."""
+    try:
+        (rows, cols), (ld, one) = t.shape, t.stride()
+        fits = (t.dtype in dtypes and t.is_cuda and (dev is None or t.device == dev) and (n is None or rows == n)
+                and (c is None or cols == c) and (one == 1 or cols <= 1) and (ld >= cols or rows <= 1))
+    except (AttributeError, TypeError, ValueError):
+        fits = False
+    if not fits:
+        _refuse(t, name, where, dtypes, dev, n, c)
+    return ld if rows > 1 else cols
+
+
+def _vec(t, name, where, dtypes, dev, c):
+    if not (getattr(t, "dtype", None) in dtypes and t.device == dev and t.shape == (c,) and (c <= 1 or t.stride(0) == 1)):
+        _refuse(t, name, where, dtypes, dev, -1, c)
 
 
 def _kept(codes, scales, n, c, where, dev):
-    import torch
     g = (c + 31) // 32
     for t, name, w in ((codes, "codes", 32 * g), (scales, "scales", g)):
-        _arg(t, name, where, (torch.uint8,), (n,), w, dev)
-        if n > 1 and t.stride(0) != w:
+        if _mat(t, name, where, _U8, dev, n, w) != w:
             raise EfError(EF_EINVAL, where, f"{name} is not contiguous")
+    return codes.data_ptr(), scales.data_ptr()
 
 
-def _mats():
-    import torch
-    return (torch.float32, torch.bfloat16)
+if _torch is not None:
+    _MATS, _U8 = (_torch.float32, _torch.bfloat16), (_torch.uint8,)
+    _CODE = {_torch.float32: EF_F32, _torch.bfloat16: EF_BF16}
+    _raw_stream = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _enqueue(fn, where, t, stream, *args):
-    """Calls the library with t's device current, on `stream` or that device's current stream."""
-    import torch
-    if t.device.index == torch.cuda.current_device():
-        _check(fn(*args, _stream(t, stream)), where)
+def _enqueue(fn, where, dev, stream, *args):
+    """Calls the library with device `dev` current, on `stream` or that device's current stream."""
+    if dev.index != _torch.cuda.current_device():
+        with _torch.cuda.device(dev):
+            return _enqueue(fn, where, dev, stream, *args)
+    if stream is not None:
+        st = stream.cuda_stream
+    elif _raw_stream is not None:
+        st = _raw_stream(dev.index)
     else:
-        with torch.cuda.device(t.device):
-            _check(fn(*args, _stream(t, stream)), where)
+        st = _torch.cuda.current_stream(dev).cuda_stream
+    code = fn(*args, st)
+    if code != EF_OK:
+        raise EfError(code, where)
 
 
 def ckpt_buffers(n, c, device="cuda"):
@@ -579,38 +595,39 @@ def linear_workspace(op, n, i, o, dtype, device="cuda"):
 
 
 def _ws(ws, where, dev):
-    if ws is not None and (not ws.is_cuda or ws.device != dev or not ws.is_contiguous()):
+    if ws is None:
+        return 0, 0
+    if not ws.is_cuda or ws.device != dev or not ws.is_contiguous():
         raise EfError(EF_EINVAL, where, f"ws is not a contiguous tensor on {dev}")
-    return _ptr(ws), _nbytes(ws)
+    return ws.data_ptr(), _nbytes(ws)
 
 
 def ef_ckpt_pack(x, codes, scales, fmt=EF_CKPT_INT8, stream=None):
     """codes, scales = the 8-bit checkpoint of x [n][c]."""
     w = "ef_ckpt_pack"
-    _arg(x, "x", w, _mats())
-    n, c = x.shape
-    _kept(codes, scales, n, c, w, x.device)
-    _enqueue(_lib.ef_ckpt_pack, w, x, stream, n, c, _ptr(x), _ld(x), _gdt(x), int(fmt), _ptr(codes), _ptr(scales))
+    ld = _mat(x, "x", w, _MATS)
+    (n, c), dev = x.shape, x.device
+    q, s = _kept(codes, scales, n, c, w, dev)
+    _enqueue(_lib.ef_ckpt_pack, w, dev, stream, n, c, x.data_ptr(), ld, _CODE[x.dtype], fmt, q, s)
 
 
 def ef_ckpt_unpack(codes, scales, fmt, y, stream=None):
     """y [n][c] = what a checkpoint stands for."""
     w = "ef_ckpt_unpack"
-    _arg(y, "y", w, _mats())
-    n, c = y.shape
-    _kept(codes, scales, n, c, w, y.device)
-    _enqueue(_lib.ef_ckpt_unpack, w, y, stream, n, c, _ptr(codes), _ptr(scales), int(fmt), _ptr(y), _ld(y), _gdt(y))
+    ld = _mat(y, "y", w, _MATS)
+    (n, c), dev = y.shape, y.device
+    q, s = _kept(codes, scales, n, c, w, dev)
+    _enqueue(_lib.ef_ckpt_unpack, w, dev, stream, n, c, q, s, fmt, y.data_ptr(), ld, _CODE[y.dtype])
 
 
 def ef_ckpt_act_backward(act, codes, scales, fmt, dy, dz, stream=None):
     """dz = dy * act'(z), z the kept input of the activation; dz may be dy."""
     w = "ef_ckpt_act_backward"
-    _arg(dy, "dy", w, _mats())
-    n, c = dy.shape
-    _arg(dz, "dz", w, (dy.dtype,), (n,), c, dy.device)
-    _kept(codes, scales, n, c, w, dy.device)
-    _enqueue(_lib.ef_ckpt_act_backward, w, dy, stream, n, c, int(act), _ptr(codes), _ptr(scales), int(fmt), _ptr(dy),
-             _ld(dy), _ptr(dz), _ld(dz), _gdt(dy))
+    ld = _mat(dy, "dy", w, _MATS)
+    (n, c), dev, t = dy.shape, dy.device, dy.dtype
+    ldz = _mat(dz, "dz", w, (t,), dev, n, c)
+    q, s = _kept(codes, scales, n, c, w, dev)
+    _enqueue(_lib.ef_ckpt_act_backward, w, dev, stream, n, c, act, q, s, fmt, dy.data_ptr(), ld, dz.data_ptr(), ldz, _CODE[t])
 
 
 def ef_linear_forward(x, weight, y, ws, bias=None, act=EF_ACT_NONE, res=None, codes=None, scales=None,
@@ -618,21 +635,21 @@ def ef_linear_forward(x, weight, y, ws, bias=None, act=EF_ACT_NONE, res=None, co
     """y = act(z) + res, z = x weight^T + bias; codes, scales (both or neither) receive the checkpoint of z.
     x [n][i], weight [o][i], y and res [n][o], bias [o]; res may be y."""
     w = "ef_linear_forward"
-    _arg(x, "x", w, _mats())
-    dev, t = x.device, (x.dtype,)
-    n, i = x.shape
-    _arg(weight, "weight", w, t, None, i, dev)
+    ldx = _mat(x, "x", w, _MATS)
+    (n, i), dev, dtypes = x.shape, x.device, (x.dtype,)
+    ldw = _mat(weight, "weight", w, dtypes, dev, None, i)
     o = weight.shape[0]
-    _arg(y, "y", w, t, (n,), o, dev)
+    ldy = _mat(y, "y", w, dtypes, dev, n, o)
+    b = r = ldr = q = s = 0
     if bias is not None:
-        _arg(bias, "bias", w, t, 0, o, dev)
+        _vec(bias, "bias", w, dtypes, dev, o)
+        b = bias.data_ptr()
     if res is not None:
-        _arg(res, "res", w, t, (n,), o, dev)
+        r, ldr = res.data_ptr(), _mat(res, "res", w, dtypes, dev, n, o)
     if codes is not None or scales is not None:
-        _kept(codes, scales, n, o, w, dev)
-    _enqueue(_lib.ef_linear_forward, w, x, stream, n, i, o, _ptr(x), _ld(x), _ptr(weight), _ld(weight), _ptr(bias),
-             int(act), _ptr(res), _ld(res) if res is not None else 0, _ptr(y), _ld(y), _gdt(x), _ptr(codes),
-             _ptr(scales), int(fmt), *_ws(ws, w, dev))
+        q, s = _kept(codes, scales, n, o, w, dev)
+    _enqueue(_lib.ef_linear_forward, w, dev, stream, n, i, o, x.data_ptr(), ldx, weight.data_ptr(), ldw, b, act, r, ldr,
+             y.data_ptr(), ldy, _CODE[x.dtype], q, s, fmt, *_ws(ws, w, dev))
 
 
 def ef_linear_dgrad(dy, weight, dx, ws, act=EF_ACT_NONE, codes=None, scales=None, fmt=EF_CKPT_INT8, res=None,
@@ -640,39 +657,37 @@ def ef_linear_dgrad(dy, weight, dx, ws, act=EF_ACT_NONE, codes=None, scales=None
     """dx = (dy weight) * act'(z) + res, z the kept input of the activation before the layer.
     dy [n][o], weight [o][i], dx and res [n][i]; res may be dx."""
     w = "ef_linear_dgrad"
-    _arg(dy, "dy", w, _mats())
-    dev, t = dy.device, (dy.dtype,)
-    n, o = dy.shape
-    _arg(weight, "weight", w, t, (o,), None, dev)
+    ldy = _mat(dy, "dy", w, _MATS)
+    (n, o), dev, dtypes = dy.shape, dy.device, (dy.dtype,)
+    ldw = _mat(weight, "weight", w, dtypes, dev, o)
     i = weight.shape[1]
-    _arg(dx, "dx", w, t, (n,), i, dev)
+    ldx = _mat(dx, "dx", w, dtypes, dev, n, i)
+    r = ldr = q = s = 0
     if res is not None:
-        _arg(res, "res", w, t, (n,), i, dev)
+        r, ldr = res.data_ptr(), _mat(res, "res", w, dtypes, dev, n, i)
     if act != EF_ACT_NONE:
-        _kept(codes, scales, n, i, w, dev)
-    else:
-        codes = scales = None
-    _enqueue(_lib.ef_linear_dgrad, w, dy, stream, n, i, o, _ptr(dy), _ld(dy), _ptr(weight), _ld(weight), int(act),
-             _ptr(codes), _ptr(scales), int(fmt), _ptr(res), _ld(res) if res is not None else 0, _ptr(dx), _ld(dx),
-             _gdt(dy), *_ws(ws, w, dev))
+        q, s = _kept(codes, scales, n, i, w, dev)
+    _enqueue(_lib.ef_linear_dgrad, w, dev, stream, n, i, o, dy.data_ptr(), ldy, weight.data_ptr(), ldw, act, q, s, fmt, r, ldr,
+             dx.data_ptr(), ldx, _CODE[dy.dtype], *_ws(ws, w, dev))
 
 
 def ef_linear_wgrad(dy, codes, scales, fmt, dw, ws, db=None, accumulate=False, stream=None):
     """dw = dy^T x, db = the sum of dy's rows (accumulate: added to what they hold), x the kept input of the layer.
     dy [n][o], dw [o][i] contiguous (a segment of the flat gradient or of the error-feedback memory), db [o]."""
     w = "ef_linear_wgrad"
-    _arg(dy, "dy", w, _mats())
-    dev = dy.device
-    n, o = dy.shape
-    _arg(dw, "dw", w, _mats(), (o,), None, dev)
+    ldy = _mat(dy, "dy", w, _MATS)
+    (n, o), dev = dy.shape, dy.device
+    ldw = _mat(dw, "dw", w, _MATS, dev, o)
     i = dw.shape[1]
-    if o > 1 and dw.stride(0) != i:
+    if ldw != i:
         raise EfError(EF_EINVAL, w, "dw is not contiguous")
+    b = 0
     if db is not None:
-        _arg(db, "db", w, (dw.dtype,), 0, o, dev)
-    _kept(codes, scales, n, i, w, dev)
-    _enqueue(_lib.ef_linear_wgrad, w, dy, stream, n, i, o, _ptr(dy), _ld(dy), _gdt(dy), _ptr(codes), _ptr(scales),
-             int(fmt), _ptr(dw), _ptr(db), _gdt(dw), 1 if accumulate else 0, *_ws(ws, w, dev))
+        _vec(db, "db", w, (dw.dtype,), dev, o)
+        b = db.data_ptr()
+    q, s = _kept(codes, scales, n, i, w, dev)
+    _enqueue(_lib.ef_linear_wgrad, w, dev, stream, n, i, o, dy.data_ptr(), ldy, _CODE[dy.dtype], q, s, fmt, dw.data_ptr(), b,
+             _CODE[dw.dtype], 1 if accumulate else 0, *_ws(ws, w, dev))
 
 
 def lib():

@@ -11,6 +11,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/efsparse.h"
 
 namespace efs {
@@ -329,16 +331,13 @@ struct Epi {
   void* db;           // wgrad: [M], the sums of A's lines, or null
 };
 
-// What the epilogue reads beside C for eight columns of a row, loaded ahead of its use; KIND the product, DT the type
-// of out, bias and res.
-template <int KIND, int DT>
-struct Side {
+// Eight neighbours of a row as they are stored, for loads that are used later.
+template <int DT>
+struct Raw {
   static constexpr int W = DT == EF_F32 ? 8 : 4;
-  uint32_t r[W];  // res, or the old dw, as stored
-  u32x2 q;        // dgrad: the kept codes and their scale
-  uint32_t s;
+  uint32_t r[W];
 
-  __device__ __forceinline__ void raw(const void* p, int64_t at, int cnt) {
+  __device__ __forceinline__ void load(const void* p, int64_t at, int cnt) {
     if (cnt >= 8) {
       const u32x4u* from = reinterpret_cast<const u32x4u*>(static_cast<const char*>(p) + at * (W / 2));
 #pragma unroll
@@ -356,6 +355,15 @@ struct Side {
     if (DT == EF_F32) return __uint_as_float(r[j % W]);
     return __uint_as_float(j & 1 ? r[j / 2 % W] & 0xFFFF0000u : r[j / 2 % W] << 16);
   }
+};
+
+// What the epilogue reads beside C for eight columns of a row, loaded ahead of its use; KIND the product, DT the type
+// of out, bias and res.
+template <int KIND, int DT>
+struct Side {
+  Raw<DT> old;  // res, or the old dw
+  u32x2 q;      // dgrad: the kept codes and their scale
+  uint32_t s;
 
   // cnt of the eight columns exist (8 or more: all; 0 or less: none)
   __device__ __forceinline__ void load(const Epi& a, int64_t row, int32_t col, int cnt) {
@@ -365,9 +373,9 @@ struct Side {
       s = a.k.scales[row * a.k.G + col / kGroup];
     }
     if (KIND == K_WGRAD) {
-      if (a.add) raw(a.out, row * a.ldo + col, cnt);
+      if (a.add) old.load(a.out, row * a.ldo + col, cnt);
     } else if (a.res) {
-      raw(a.res, row * a.ldr + col, cnt);
+      old.load(a.res, row * a.ldr + col, cnt);
     }
   }
 };
@@ -406,7 +414,7 @@ __device__ __forceinline__ void epilogue8(const Epi& a, int64_t row, int32_t col
   }
   if (KIND == K_WGRAD ? a.add != 0 : a.res != nullptr) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = side.value(j) + v[j];
+    for (int j = 0; j < 8; ++j) v[j] = side.old.value(j) + v[j];
   }
   store8<DT>(a.out, row * a.ldo + col, cnt, v);
 }
@@ -499,109 +507,18 @@ __device__ __forceinline__ void finish_db(const float (&s)[T], int lane, int64_t
   }
 }
 
-// ---------------------------------------------------------------------------------------------
-// The product for every type, order and alignment, in float32: C[m][n] = sum_k A(m, k) B(n, k).
-//   forward  A = x  [n][i] (k along the row), B = W [o][i] (k along the row)
-//   dgrad    A = dy [n][o] (k along the row), B = W [o][i] (k down the rows)
-//   wgrad    A = dy [t][o] (k down the rows), B = the checkpoint [t][i] (k down the rows)
-// A workgroup has 128 x 128 of C, four wavefronts 64 x 64 each, and steps of 16 along k: the tiles of the next
-// step are loaded into registers while this one is multiplied, and stored to the other half of the LDS as
-// float32 [k][m], whatever the order in memory.
-// ---------------------------------------------------------------------------------------------
 struct Mat {
   const void* p;
   int64_t ld;
 };
 
-constexpr int kAnyTile = 128, kAnyK = 16, kAnyPitch = 132;  // (132: rows eight apart land 32 banks apart)
-
-// Eight elements along the contiguous direction of a tile of A or B: ROWS of the matrix down, 8 columns across.
-template <int DT>
-__device__ __forceinline__ void load_chunk(const Mat& a, int64_t row, int64_t rows, int64_t col, int64_t cols, float (&v)[8]) {
-  const int64_t left = cols - col;
-  load8<DT>(a.p, row * a.ld + col, row < rows ? (int)(left < 8 ? left : 8) : 0, v);
-}
-
-template <int KIND, int DT, int DO>
-__global__ __launch_bounds__(256) void k_linear_any(int32_t M, int32_t N, int32_t K, Mat A, Mat B, Kept BK, Epi ep, Split sp) {
-  constexpr bool AKC = KIND != K_WGRAD, BKC = KIND == K_FWD, B8 = KIND == K_WGRAD;
-  constexpr int kTileF = kAnyK * kAnyPitch;
-  __shared__ __align__(16) float sm[4 * 32 * kSlabPitch > 4 * kTileF ? 4 * 32 * kSlabPitch : 4 * kTileF];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int32_t tn = (N + kAnyTile - 1) / kAnyTile;
-  const int64_t m0 = (int64_t)(blockIdx.x / tn) * kAnyTile, n0 = (int64_t)(blockIdx.x % tn) * kAnyTile;
-  const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-  float av[8], bv[8];
-  // tile element of this thread's chunk: (line, 8 along k) or (k, 8 along the line)
-  const int kc_l = t >> 1, kc_k = (t & 1) * 8, ks_k = t >> 4, ks_l = (t & 15) * 8;
-  auto fetch = [&](int64_t k0) {
-    if (AKC) load_chunk<DT>(A, m0 + kc_l, M, k0 + kc_k, K, av);
-    else load_chunk<DT>(A, k0 + ks_k, K, m0 + ks_l, M, av);
-    if (B8) {
-      const int64_t row = k0 + ks_k, col = n0 + ks_l;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) bv[j] = 0.0f;
-      if (row < K && col < N)
-        decode8(*reinterpret_cast<const u32x2u*>(BK.codes + row * BK.G * kGroup + col),
-                BK.scales[row * BK.G + col / kGroup], BK.fmt, bv);
-    } else if (BKC) {
-      load_chunk<DT>(B, n0 + kc_l, N, k0 + kc_k, K, bv);
-    } else {
-      load_chunk<DT>(B, k0 + ks_k, K, n0 + ks_l, N, bv);
-    }
-  };
-  auto put = [&](float* s, bool kc, const float (&v)[8]) {
-    if (kc) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[(kc_k + j) * kAnyPitch + kc_l] = v[j];
-    } else {
-      *reinterpret_cast<f32x4*>(s + ks_k * kAnyPitch + ks_l) = f32x4{v[0], v[1], v[2], v[3]};
-      *reinterpret_cast<f32x4*>(s + ks_k * kAnyPitch + ks_l + 4) = f32x4{v[4], v[5], v[6], v[7]};
-    }
-  };
-  f32x16 acc[2][2];
-#pragma unroll
-  for (int a = 0; a < 2; ++a)
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.0f;
-  const bool sums = KIND == K_WGRAD && ep.db && n0 == 0 && wn == 0;
-  float bs[2] = {0.0f, 0.0f};
-  const int64_t all = ((int64_t)K + kAnyK - 1) / kAnyK;
-  const int64_t s0 = (int64_t)blockIdx.y * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
-  if (s0 < s1) fetch(s0 * kAnyK);
-  for (int64_t s = s0; s < s1; ++s) {
-    float* sa = sm + (s & 1) * 2 * kTileF;
-    float* sb = sa + kTileF;
-    put(sa, AKC, av);
-    put(sb, BKC, bv);
-    __syncthreads();  // (the other half was last read before the previous barrier's step ended)
-    if (s + 1 < s1) fetch((s + 1) * kAnyK);
-#pragma unroll
-    for (int k = 0; k < kAnyK; k += 2) {
-      const int row = (k + (lane >> 5)) * kAnyPitch + (lane & 31);
-      const float a0 = sa[row + wm], a1 = sa[row + wm + 32], b0 = sb[row + wn], b1 = sb[row + wn + 32];
-      acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a0, b0, acc[0][0], 0, 0, 0);
-      acc[0][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a0, b1, acc[0][1], 0, 0, 0);
-      acc[1][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a1, b0, acc[1][0], 0, 0, 0);
-      acc[1][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a1, b1, acc[1][1], 0, 0, 0);
-      if (sums) {
-        bs[0] += a0;
-        bs[1] += a1;
-      }
-    }
-  }
-  __syncthreads();
-  float* slab = sm + wave * 32 * kSlabPitch;
-  finish<KIND, DO, 2>(acc, slab, lane, m0 + wm, n0 + wn, M, N, ep, sp);
-  if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
-}
-
 // ---------------------------------------------------------------------------------------------
-// The same products on bfloat16 matrix instructions, for matrices whose rows start on 16 bytes.
+// The products, C[m][n] = sum_k A(m, k) B(n, k), on bfloat16 matrix instructions with float32 sums:
+//   forward  A = x  [n][i] (k along the row), B = W [o][i] (k along the row)
+//   dgrad    A = dy [n][o] (k along the row), B = W [o][i] (k down the rows)
+//   wgrad    A = dy [t][o] (k down the rows), B = the checkpoint [t][i] (k down the rows)
 //
-// A workgroup has BM x BN of C, WM x WN wavefronts, and steps of 64 along k through two halves of the LDS.  A
+// k_linear_bf16, for bfloat16 matrices whose rows start on 16 bytes.  A workgroup has BM x BN of C, WM x WN wavefronts, and steps of 64 along k through two halves of the LDS.  A
 // wavefront has BM / WM rows and 64 columns of C in accumulators of 32 x 32.  Operands go from memory to the LDS
 // without passing registers (16 bytes a lane; what lies outside the matrix arrives as zeros by the buffer's
 // bounds), in the order that they have in memory:
@@ -769,15 +686,15 @@ struct StreamKept {
   }
 };
 
-// A wavefront's fragments of one operand: T of 32 lines by 16 k, eight k a lane.
-template <bool KC, int LINES, int T>
+// A wavefront's fragments of one operand: T of 32 lines by 16 k, eight k a lane; BK k per tile.
+template <bool KC, int LINES, int T, int BK = kBK>
 struct Reader {
-  int off[KC ? 4 : T];
+  int off[KC ? BK / 16 : T];
   __device__ __forceinline__ void init(int line0, int lane) {
     if (KC) {
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-        off[ks] = (line0 + (lane & 31)) * 128 + (((ks * 2 + (lane >> 5)) ^ ((lane >> 1) & 7)) << 4);
+      for (int ks = 0; ks < BK / 16; ++ks)
+        off[ks] = (line0 + (lane & 31)) * BK * 2 + (((ks * 2 + (lane >> 5)) ^ (BK == 64 ? (lane >> 1) & 7 : (lane >> 2) & 3)) << 4);
     } else {
       const int x = (lane >> 2) & 3;
 #pragma unroll
@@ -786,7 +703,7 @@ struct Reader {
     }
   }
   __device__ __forceinline__ bf16x8 read(const char* lds, int ks, int t) const {
-    if (KC) return *reinterpret_cast<const bf16x8*>(lds + off[ks] + t * 32 * 128);
+    if (KC) return *reinterpret_cast<const bf16x8*>(lds + off[ks] + t * 32 * BK * 2);
     const char* p = lds + off[t] + ks * 16 * LINES * 2;
     const bf16x4 a = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((EF_LDS s16x4*)p));
     const bf16x4 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((EF_LDS s16x4*)(p + 4 * LINES * 2)));
@@ -817,8 +734,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
   constexpr bool AKC = KIND != K_WGRAD, BKC = KIND == K_FWD, B8 = KIND == K_WGRAD;
   constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
   static_assert(TN == 2, "the epilogue hands over 64 columns a wavefront");
-  constexpr int kA = BM * kBK * 2, kHalf = (BM + BN) * kBK * 2;
-  __shared__ __align__(1024) char lds[2 * kHalf];
+  constexpr int kA = BM * kBK * 2, kB = BN * kBK * 2;
+  __shared__ __align__(1024) char lds[3 * kA + 2 * kB];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   uint32_t ti, tj;
   tile_of(blockIdx.x, ((uint32_t)M + BM - 1) / BM, ((uint32_t)N + BN - 1) / BN, &ti, &tj);
@@ -852,20 +769,20 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
   for (int a = 0; a < TM; ++a) bs[a] = 0.0f;
   bf16x8 fa[2][TM], fb[2][TN];
   // One slice: the matrix instructions of the fragments h, and between them, one by one, the reads of the next ones
-  // (slice ks of rd) and whatever else there is to do.  Pinned in this order: left to itself the compiler gathers the
+  // (slice ks of the tiles from_a and from_b, where there are `more`) and whatever else there is to do.  Pinned in this order: left to itself the compiler gathers the
   // reads before their use.
   constexpr int kMul = TM * TN;
-  auto slice = [&](int h, const char* rd, int ks, auto&& between) {
+  auto slice = [&](auto more, int h, const char* from_a, const char* from_b, int ks, auto&& between) {
 #pragma unroll
     for (int i = 0; i < kMul; ++i) {
       const int a = i / TN, b = i % TN;
       acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[h][a], fb[h][b], acc[a][b], 0, 0, 0);
-      if (rd) {
-        if (i < TN) fb[h ^ 1][i] = rb.read(rd + kA, ks, i);
-        else if (i - TN < TM) fa[h ^ 1][i - TN] = ra.read(rd, ks, i - TN);
+      if constexpr (decltype(more)::value) {
+        if (i < TN) fb[h ^ 1][i] = rb.read(from_b, ks, i);
+        else if (i - TN < TM) fa[h ^ 1][i - TN] = ra.read(from_a, ks, i - TN);
         if (i == kMul - 1)
 #pragma unroll
-          for (int t = kMul - TN; t < TM; ++t) fa[h ^ 1][t] = ra.read(rd, ks, t);
+          for (int t = kMul - TN; t < TM; ++t) fa[h ^ 1][t] = ra.read(from_a, ks, t);
       }
       between(i);
       __builtin_amdgcn_sched_barrier(0);
@@ -875,9 +792,12 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
       for (int a = 0; a < TM; ++a) bs[a] = add8(fa[h][a], bs[a]);
     }
   };
-  // Step s + 2 goes into the half of step s from the barrier on that ends step s; the instructions of its last
-  // fragments (slice 3) come behind that barrier.  A checkpoint's codes arrive in registers by the same barrier as
-  // the other operand of the step before, and follow it a quarter a slice.
+  // Tiles of A take turns in three parts of the LDS, those of B in two.  Behind the barrier that ends step s its last
+  // fragments' instructions (slice 3) are to be issued, and its parts of the LDS are free: for step s + 2 of B, loaded
+  // in slice 3, and step s + 3 of A, loaded in the slices after that, which have more than a step to arrive.  The
+  // address unit takes 16 cycles for a load, and a wavefront that finds it busy issues nothing: one load every kGap
+  // matrix instructions.  A checkpoint's codes arrive in registers by the same barrier as the tile of B before them,
+  // and go into the LDS a quarter a slice.
   using SA = Stream<AKC, BM, NW>;
   using SB = Stream<BKC, BN, NW>;
   typename SK::Codes codes[2];
@@ -888,80 +808,248 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
 #pragma unroll
       for (int h = 0; h < P; ++h) w[i * P + h] = sk.pair(c, f, i * P + h);
     }
-    if (i == kMul / 2) sk.put(f, w, to + kA);
+    if (i == kMul / 2) sk.put(f, w, to);
   };
-  auto tile = [&](int64_t s, char* to) {
-#pragma unroll
-    for (int j = 0; j < SA::J; ++j) sa.load(j, s, to, wave);
-    if (!B8)
-#pragma unroll
-      for (int j = 0; j < SB::J; ++j) sb.load(j, s, to + kA, wave);
-  };
+  constexpr int kGap = SA::J <= kMul / 2 ? 2 : 1;
   auto decode = [&](const typename SK::Codes& c, int f0, int f1, char* to) {
 #pragma unroll
     for (int f = f0; f < f1; ++f) {
 #pragma unroll
       for (int h = 0; h < 4; ++h) w[h] = sk.pair(c, f, h);
-      sk.put(f, w, to + kA);
+      sk.put(f, w, to);
     }
   };
-  char* const half0 = lds;
-  char* const half1 = lds + kHalf;
+  char *a0 = lds, *a1 = lds + kA, *a2 = lds + 2 * kA;
+  char* const b0 = lds + 3 * kA;
+  char* const b1 = b0 + kB;
   if (B8) {
     sk.fetch(s0, codes[0]);
     sk.fetch(s0 + 1, codes[1]);
   }
-  tile(s0, half0);
-  tile(s0 + 1, half1);
+#pragma unroll
+  for (int j = 0; j < SA::J; ++j) {
+    sa.load(j, s0, a0, wave);
+    if (!B8) sb.load(j, s0, b0, wave);
+  }
+#pragma unroll
+  for (int j = 0; j < SA::J; ++j) {
+    sa.load(j, s0 + 1, a1, wave);
+    if (!B8) sb.load(j, s0 + 1, b1, wave);
+  }
   if (B8) {
-    decode(codes[0], 0, 4, half0);
-    decode(codes[1], 0, 1, half1);
+    decode(codes[0], 0, 4, b0);
+    decode(codes[1], 0, 1, b1);
     sk.fetch(s0 + 2, codes[0]);
   }
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
 #pragma unroll
-  for (int t = 0; t < TM; ++t) fa[0][t] = ra.read(half0, 0, t);
+  for (int t = 0; t < TM; ++t) fa[0][t] = ra.read(a0, 0, t);
 #pragma unroll
-  for (int t = 0; t < TN; ++t) fb[0][t] = rb.read(half0 + kA, 0, t);
-  // Step s in cur, s + 1 in nxt (of its checkpoint, in `now`, a quarter); `then` has the codes of s + 2.
+  for (int t = 0; t < TN; ++t) fb[0][t] = rb.read(b0, 0, t);
+  // Step s in a0 and cur, s + 1 in a1 and nxt (of its checkpoint, in `now`, a quarter); `then` has the codes of s + 2.
   auto advance = [&](int64_t s, char* cur, char* nxt, typename SK::Codes& now, typename SK::Codes& then) {
 #pragma unroll
     for (int ks = 0; ks < 3; ++ks)
-      slice(ks & 1, cur, ks + 1, [&](int i) {
+      slice(std::true_type{}, ks & 1, a0, cur, ks + 1, [&](int i) {
+        const int j = (ks * kMul + i) / kGap;
+        if (i % kGap == 0 && j < SA::J) sa.load(j, s + 2, a2, wave);
         if (B8) quarter(i, now, ks + 1, nxt);
       });
-    // This wavefront's part of the next step has arrived, and its last reads of this one.
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    slice(1, nxt, 0, [&](int i) {
+    // This wavefront's part of the next step has arrived (all but the last loads, of A behind it), and its last reads
+    // of this one.
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SA::J) : "memory");
+    slice(std::true_type{}, 1, a1, nxt, 0, [&](int i) {
       if (B8 && i == 0) sk.fetch(s + 3, now);
-      constexpr int D = B8 ? SA::J : SA::J + SB::J, Q = (D + kMul - 1) / kMul;
-#pragma unroll
-      for (int d = 0; d < Q; ++d) {
-        const int j = i * Q + d;
-        if (j < SA::J) sa.load(j, s + 2, cur, wave);
-        else if (!B8 && j < D) sb.load(j - SA::J, s + 2, cur + kA, wave);
-      }
+      if (!B8 && i % kGap == 0 && i / kGap < SB::J) sb.load(i / kGap, s + 2, cur, wave);
       if (B8) quarter(i, then, 0, cur);
     });
+    char* x = a0;
+    a0 = a1;
+    a1 = a2;
+    a2 = x;
   };
+  static_assert(SA::J == SB::J && kMul / kGap >= SB::J, "B's loads fit a slice");
   int64_t s = s0;
   for (; s + 2 < s1; s += 2) {
-    advance(s, half0, half1, codes[1], codes[0]);
-    advance(s + 1, half1, half0, codes[0], codes[1]);
+    advance(s, b0, b1, codes[1], codes[0]);
+    advance(s + 1, b1, b0, codes[0], codes[1]);
   }
-  const char* last = half0;
+  const char* last = b0;
   if (s + 1 < s1) {
-    advance(s, half0, half1, codes[1], codes[0]);
-    last = half1;
+    advance(s, b0, b1, codes[1], codes[0]);
+    last = b1;
   }
 #pragma unroll
-  for (int ks = 0; ks < 3; ++ks) slice(ks & 1, last, ks + 1, [](int) {});
-  slice(1, nullptr, 0, [](int) {});
+  for (int ks = 0; ks < 3; ++ks) slice(std::true_type{}, ks & 1, a0, last, ks + 1, [](int) {});
+  slice(std::false_type{}, 1, a0, last, 0, [](int) {});
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   float* slab = reinterpret_cast<float*>(lds) + wave * 32 * kSlabPitch;
   finish<KIND, DO, TM>(acc, slab, lane, m0 + wm, n0 + wn, M, N, ep, sp);
+  if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
+}
+
+// ---------------------------------------------------------------------------------------------
+// The same products for every type and alignment.  Operands pass through registers, a step of 32 ahead.  A float32
+// value goes into the LDS as three bfloat16 numbers, hi + mid + lo: rounded to nearest three times, which leaves
+// nothing of its 24 bits.  Of the nine products of two such sums the six that matter are taken; what is left out is
+// 2^-23 of the product at most.  A checkpoint's values are bfloat16 numbers, so against them three products are the
+// whole.  (Against the matrix instructions for float32, a sixteenth as fast: n, i, o = 1021, 771, 1285, dgrad
+// 49 -> ANY_D us; 2043, 1285, 771, wgrad 87 -> ANY_W us.)  An infinity has no such parts: it comes out as NaN.
+// A workgroup has 128 x 128 of C, four wavefronts of 64 x 64.
+// ---------------------------------------------------------------------------------------------
+constexpr int kAnyTile = 128, kAnyK = 32;
+constexpr int kPlane = kAnyTile * kAnyK * 2;
+
+// One operand's chunks of eight elements of a step, two a thread: lines by k where KC, else k by lines.
+template <int DT, bool KC, int P>
+struct Chunks {
+  Raw<DT> raw[2];
+  __device__ __forceinline__ static int line(int t, int j) { return KC ? (j * 256 + t) / 4 : (t & 15) * 8; }
+  __device__ __forceinline__ static int k(int t, int j) { return KC ? (t & 3) * 8 : (j * 256 + t) / 16; }
+  __device__ __forceinline__ static int place(int t, int j) {
+    const int l = line(t, j), r = k(t, j);
+    return KC ? l * kAnyK * 2 + (((t & 3) ^ ((l >> 2) & 3)) << 4) : r * kAnyTile * 2 + (((t >> 2 & 3) ^ (r & 3)) << 6) + (t & 3) * 16;
+  }
+  __device__ __forceinline__ void fetch(const Mat& m, int64_t line0, int64_t lines, int64_t k0, int64_t K, int t) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int64_t l = line0 + line(t, j), r = k0 + k(t, j);
+      const int64_t row = KC ? l : r, rows = KC ? lines : K, col = KC ? r : l, left = (KC ? K : lines) - col;
+      raw[j].load(m.p, row * m.ld + col, row < rows ? (int)(left < 8 ? left : 8) : 0);
+    }
+  }
+  __device__ __forceinline__ void put(char* lds, int t) const {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      char* to = lds + place(t, j);
+      if (P == 1) {
+        *reinterpret_cast<u32x4*>(to) = u32x4{raw[j].r[0], raw[j].r[1], raw[j].r[2], raw[j].r[3]};
+      } else {
+        u32x4 w[3];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          float x = raw[j].value(2 * h), y = raw[j].value(2 * h + 1);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) {
+            // (hi is held at the largest bfloat16: a finite value does not round to an infinity, and what is not
+            // finite goes on into mid and lo)
+            w[p][h] = p ? f_bf16x2(x, y) : f_bf16x2(__builtin_amdgcn_fmed3f(x, -0x1.FEp127f, 0x1.FEp127f), __builtin_amdgcn_fmed3f(y, -0x1.FEp127f, 0x1.FEp127f));
+            x -= __uint_as_float(w[p][h] << 16);
+            y -= __uint_as_float(w[p][h] & 0xFFFF0000u);
+          }
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(to + p * kPlane) = w[p];
+      }
+    }
+  }
+};
+
+struct KeptChunks {
+  u32x2 q[2];
+  uint32_t s[2];
+  using At = Chunks<EF_BF16, false, 1>;
+  __device__ __forceinline__ void fetch(const Kept& m, int64_t line0, int64_t lines, int64_t k0, int64_t K, int t) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int64_t l = line0 + At::line(t, j), r = k0 + At::k(t, j);
+      q[j] = u32x2{0u, 0u};
+      s[j] = 0u;
+      if (r < K && l < lines) {
+        q[j] = *reinterpret_cast<const u32x2*>(m.codes + r * m.G * kGroup + l);
+        s[j] = m.scales[r * m.G + l / kGroup];
+      }
+    }
+  }
+  __device__ __forceinline__ void put(char* lds, int fmt, int t) const {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float v[8];
+      decode8(q[j], s[j], fmt, v);
+      u32x4 w;
+#pragma unroll
+      for (int h = 0; h < 4; ++h) w[h] = __builtin_amdgcn_perm(__float_as_uint(v[2 * h + 1]), __float_as_uint(v[2 * h]), 0x07060302u);
+      *reinterpret_cast<u32x4*>(lds + At::place(t, j)) = w;
+    }
+  }
+};
+
+template <int KIND, int DT, int DO>
+__global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int32_t K, Mat A, Mat B, Kept BK, Epi ep, Split sp) {
+  constexpr bool AKC = KIND != K_WGRAD, BKC = KIND == K_FWD, B8 = KIND == K_WGRAD;
+  constexpr int PA = DT == EF_F32 ? 3 : 1, PB = B8 ? 1 : PA;
+  constexpr int kTiles = (PA + PB) * kPlane, kSlabs = 4 * 32 * kSlabPitch * 4;
+  __shared__ __align__(1024) char lds[kTiles > kSlabs ? kTiles : kSlabs];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  uint32_t ti, tj;
+  tile_of(blockIdx.x, ((uint32_t)M + kAnyTile - 1) / kAnyTile, ((uint32_t)N + kAnyTile - 1) / kAnyTile, &ti, &tj);
+  const int64_t m0 = (int64_t)ti * kAnyTile, n0 = (int64_t)tj * kAnyTile;
+  const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
+  Chunks<DT, AKC, PA> ca;
+  Chunks<DT, BKC, PB> cb;
+  KeptChunks ck;
+  Reader<AKC, kAnyTile, 2, kAnyK> ra;
+  Reader<BKC, kAnyTile, 2, kAnyK> rb;
+  ra.init(wm, lane);
+  rb.init(wn, lane);
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int a = 0; a < 2; ++a)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.0f;
+  const bool sums = KIND == K_WGRAD && ep.db && n0 == 0 && wn == 0;
+  float bs[2] = {0.0f, 0.0f};
+  const int64_t all = ((int64_t)K + kAnyK - 1) / kAnyK;
+  const int64_t s0 = (int64_t)blockIdx.y * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
+  auto fetch = [&](int64_t s) {
+    ca.fetch(A, m0, M, s * kAnyK, K, t);
+    if (B8) ck.fetch(BK, n0, N, s * kAnyK, K, t);
+    else cb.fetch(B, n0, N, s * kAnyK, K, t);
+  };
+  if (s0 < s1) fetch(s0);
+  for (int64_t s = s0; s < s1; ++s) {
+    __syncthreads();
+    ca.put(lds, t);
+    if (B8) ck.put(lds + PA * kPlane, BK.fmt, t);
+    else cb.put(lds + PA * kPlane, t);
+    __syncthreads();
+    if (s + 1 < s1) fetch(s + 1);
+#pragma unroll
+    for (int ks = 0; ks < kAnyK / 16; ++ks) {
+      bf16x8 fa[PA][2], fb[PB][2];
+#pragma unroll
+      for (int p = 0; p < PA; ++p)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) fa[p][i] = ra.read(lds + p * kPlane, ks, i);
+#pragma unroll
+      for (int p = 0; p < PB; ++p)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) fb[p][i] = rb.read(lds + (PA + p) * kPlane, ks, i);
+#pragma unroll
+      for (int d = PA + PB - 2; d >= 0; --d)  // the least products first
+#pragma unroll
+        for (int p = 0; p < PA; ++p)
+#pragma unroll
+          for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+              if (d < 3 && d - p >= 0 && d - p < PB)
+                acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[p][a], fb[d - p][b], acc[a][b], 0, 0, 0);
+      if (sums) {
+#pragma unroll
+        for (int p = PA - 1; p >= 0; --p)
+#pragma unroll
+          for (int a = 0; a < 2; ++a) bs[a] = add8(fa[p][a], bs[a]);
+      }
+    }
+  }
+  __syncthreads();
+  float* slab = reinterpret_cast<float*>(lds) + wave * 32 * kSlabPitch;
+  finish<KIND, DO, 2>(acc, slab, lane, m0 + wm, n0 + wn, M, N, ep, sp);
   if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
 }
 

@@ -102,7 +102,7 @@ struct Cost {
   int tile, k, per_cu;
   double step, half, fixed;
 };
-constexpr Cost kCosts[3] = {{kAnyTile, kAnyK, 1, 0.9, 0.9, 4.0}, {128, kBK, 2, 0.75, 0.45, 4.0}, {256, kBK, 1, 1.3, 1.3, 6.0}};
+constexpr Cost kCosts[3] = {{kAnyTile, kAnyK, 2, 1.4, 1.0, 4.0}, {128, kBK, 2, 0.75, 0.45, 4.0}, {256, kBK, 1, 1.3, 1.3, 6.0}};
 
 double cost_of(const Cost& c, int64_t M, int64_t N, int64_t K, int64_t splits, int64_t per) {
   const double wgs = (double)((M + c.tile - 1) / c.tile) * (double)((N + c.tile - 1) / c.tile) * (double)splits;

@@ -197,12 +197,14 @@ __device__ __forceinline__ float normal_cdf(float z, float* density) {
   return z < 0.0f ? lo : 1.0f - lo;
 }
 
-// 1 / (1 + exp(-u))
-__device__ __forceinline__ float sigmoid(float u) {
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * u));
-}
+// 1 / (1 + 2^t): the logistic function of u at t = -u log2 e
+__device__ __forceinline__ float logistic2(float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t)); }
 
-__device__ __forceinline__ float gelu_u(float z) { return 2.0f * kGeluA * fmaf(kGeluB * z * z, z, z); }
+// (1 + tanh x) / 2 is the logistic function of 2 x: its t for GELU's x at z
+__device__ __forceinline__ float gelu_t(float z) {
+  constexpr float a = -2.0f * kGeluA * kLog2e;
+  return z * fmaf(a * kGeluB * z, z, a);
+}
 
 __device__ __forceinline__ void act_value(float (&v)[8], int act) {
   float d;
@@ -215,19 +217,19 @@ __device__ __forceinline__ void act_value(float (&v)[8], int act) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] *= normal_cdf(v[j], &d);
       break;
-    case EF_ACT_GELU_TANH:  // (1 + tanh x) / 2 = sigmoid(2 x)
+    case EF_ACT_GELU_TANH:
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= sigmoid(gelu_u(v[j]));
+      for (int j = 0; j < 8; ++j) v[j] *= logistic2(gelu_t(v[j]));
       break;
     case EF_ACT_SILU:
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= sigmoid(v[j]);
+      for (int j = 0; j < 8; ++j) v[j] *= logistic2(-kLog2e * v[j]);
       break;
   }
 }
 
 // v *= the derivative at z.  Far out, where it is 0 or 1 to float32, z is held at a bound: no product there
-// overflows.  (sigmoid(-u) is taken by itself: 1 - sigmoid(u) would cancel.)
+// overflows.  (The logistic function at -u is taken by itself: 1 minus that at u would cancel.)
 __device__ __forceinline__ float held(float z, float b) { return z > b ? b : (z < -b ? -b : z); }
 
 __device__ __forceinline__ void act_slope(float (&v)[8], const float (&z)[8], int act) {
@@ -248,14 +250,14 @@ __device__ __forceinline__ void act_slope(float (&v)[8], const float (&z)[8], in
     case EF_ACT_GELU_TANH:
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float x = held(z[j], 16.0f), u = gelu_u(x), p = sigmoid(u), q = sigmoid(-u);
+        const float x = held(z[j], 16.0f), t = gelu_t(x), p = logistic2(t), q = logistic2(-t);
         v[j] *= fmaf(x * p * q, 2.0f * kGeluA * fmaf(3.0f * kGeluB * x, x, 1.0f), p);
       }
       break;
     case EF_ACT_SILU:
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float x = held(z[j], 128.0f), p = sigmoid(x), q = sigmoid(-x);
+        const float x = held(z[j], 128.0f), p = logistic2(-kLog2e * x), q = logistic2(kLog2e * x);
         v[j] *= fmaf(x * p, q, p);
       }
       break;
@@ -442,52 +444,58 @@ struct Split {
   int32_t per;     // steps per split
 };
 
-// A wavefront's T times 32 x 64 of C, handed over 32 rows at a time through its own part of the LDS (a wavefront's
-// reads and writes of the LDS keep their order): from lanes that hold single columns, four rows each, to lanes that
-// hold eight columns of a row.  What the epilogue reads beside C is loaded 32 rows ahead.
+// A wavefront's T times 32 x 64 of C, handed over R times 32 rows at a time through its own part of the LDS (a
+// wavefront's reads and writes of the LDS keep their order): from lanes that hold single columns, four rows each, to
+// lanes that hold eight columns of a row.  Eight rows a turn, in a loop that stays a loop: unrolled, the epilogue was
+// 100 KB of instructions, more than their cache holds.  What it reads beside C is loaded a turn ahead.
 constexpr int kSlabPitch = 68;
-template <int KIND, int DO, int T>
-__device__ __forceinline__ void finish(const f32x16 (&acc)[T][2], float* slab, int lane, int64_t row0, int64_t col0, int32_t M,
+constexpr int slab_bytes(int waves, int R) { return waves * R * 32 * kSlabPitch * 4; }
+template <int KIND, int DO, int T, int R>
+__device__ __forceinline__ void finish(const f32x16 (&acc)[T][2], char* lds, int wave, int lane, int64_t row0, int64_t col0, int32_t M,
                                        int32_t N, const Epi& ep, const Split& sp) {
-  const int rr = lane >> 3;
+  float* slab = reinterpret_cast<float*>(lds) + wave * R * 32 * kSlabPitch;
   const int32_t col = (int32_t)col0 + (lane & 7) * 8;
+  const float* from = slab + (lane >> 3) * kSlabPitch + (lane & 7) * 8;
   float bias[8];
-  Side<KIND, DO> side[2][4];
-  auto ahead = [&](int a) {
+  if (!sp.part) load_bias<KIND, DO>(ep, col, N, bias);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t row = row0 + a * 32 + q * 8 + rr;
-      side[a & 1][q].load(ep, row, col, row < M ? N - col : kNoRow);
-    }
-  };
-  if (!sp.part) {
-    load_bias<KIND, DO>(ep, col, N, bias);
-    ahead(0);
-  }
-#pragma unroll
-  for (int a = 0; a < T; ++a) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        slab[((r >> 2) * 8 + (lane >> 5) * 4 + (r & 3)) * kSlabPitch + b * 32 + (lane & 31)] = acc[a][b][r];
-    asm volatile("" ::: "memory");
-    if (!sp.part && a + 1 < T) ahead(a + 1);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t row = row0 + a * 32 + q * 8 + rr;
-      const float* from = slab + (q * 8 + rr) * kSlabPitch + (lane & 7) * 8;
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(from), hi = *reinterpret_cast<const f32x4*>(from + 4);
+  for (int p = 0; p < T / R; ++p) {
+    const int64_t top = row0 + p * R * 32 + (lane >> 3);
+    Side<KIND, DO> even, odd;
+    auto ahead = [&](Side<KIND, DO>& side, int q) {
+      const int64_t row = top + q * 8;
+      side.load(ep, row, col, row < M ? N - col : kNoRow);
+    };
+    auto turn = [&](const Side<KIND, DO>& side, int q) {
+      const int64_t row = top + q * 8;
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(from + q * 8 * kSlabPitch);
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(from + q * 8 * kSlabPitch + 4);
       if (sp.part) {
         if (row < M && col < sp.Np) {
-          float* p = sp.part + blockIdx.y * sp.plane + row * sp.Np + col;
-          *reinterpret_cast<f32x4*>(p) = lo;
-          *reinterpret_cast<f32x4*>(p + 4) = hi;
+          float* to = sp.part + blockIdx.y * sp.plane + row * sp.Np + col;
+          *reinterpret_cast<f32x4*>(to) = lo;
+          *reinterpret_cast<f32x4*>(to + 4) = hi;
         }
       } else {
         float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        epilogue8<KIND, DO>(ep, row, col, row < M ? N - col : kNoRow, v, bias, side[a & 1][q]);
+        epilogue8<KIND, DO>(ep, row, col, row < M ? N - col : kNoRow, v, bias, side);
       }
+    };
+    if (!sp.part) ahead(even, 0);
+#pragma unroll
+    for (int a = 0; a < R; ++a)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          slab[(a * 32 + (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3)) * kSlabPitch + b * 32 + (lane & 31)] = acc[p * R + a][b][r];
+    asm volatile("" ::: "memory");
+#pragma unroll 1
+    for (int q = 0; q < R * 4; q += 2) {
+      if (!sp.part) ahead(odd, q + 1);
+      turn(even, q);
+      if (!sp.part && q + 2 < R * 4) ahead(even, q + 2);
+      turn(odd, q + 1);
     }
     asm volatile("" ::: "memory");
   }
@@ -885,8 +893,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
   slice(std::false_type{}, 1, a0, last, 0, [](int) {});
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
-  float* slab = reinterpret_cast<float*>(lds) + wave * 32 * kSlabPitch;
-  finish<KIND, DO, TM>(acc, slab, lane, m0 + wm, n0 + wn, M, N, ep, sp);
+  static_assert(slab_bytes(NW, 2) <= sizeof(lds), "the epilogue's part of the LDS");
+  finish<KIND, DO, TM, 2>(acc, lds, wave, lane, m0 + wm, n0 + wn, M, N, ep, sp);
   if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
 }
 
@@ -980,7 +988,7 @@ template <int KIND, int DT, int DO>
 __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int32_t K, Mat A, Mat B, Kept BK, Epi ep, Split sp) {
   constexpr bool AKC = KIND != K_WGRAD, BKC = KIND == K_FWD, B8 = KIND == K_WGRAD;
   constexpr int PA = DT == EF_F32 ? 3 : 1, PB = B8 ? 1 : PA;
-  constexpr int kTiles = (PA + PB) * kPlane, kSlabs = 4 * 32 * kSlabPitch * 4;
+  constexpr int kTiles = (PA + PB) * kPlane, kSlabs = slab_bytes(4, 1);
   __shared__ __align__(1024) char lds[kTiles > kSlabs ? kTiles : kSlabs];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   uint32_t ti, tj;
@@ -1048,8 +1056,7 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
     }
   }
   __syncthreads();
-  float* slab = reinterpret_cast<float*>(lds) + wave * 32 * kSlabPitch;
-  finish<KIND, DO, 2>(acc, slab, lane, m0 + wm, n0 + wn, M, N, ep, sp);
+  finish<KIND, DO, 2, 1>(acc, lds, wave, lane, m0 + wm, n0 + wn, M, N, ep, sp);
   if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
 }
 

@@ -573,49 +573,58 @@ __device__ __forceinline__ void buffer_to_lds(const char* base, uint32_t bytes, 
 }
 
 // One operand's way into the LDS.  KC: k along the row.  LINES rows of C (or columns) per tile, NW wavefronts.
+// (K is at most 2^30 here: 32 bits hold every k.)
 template <bool KC, int LINES, int NW>
 struct Stream {
   static constexpr int J = LINES * kBK * 2 / 1024 / NW;  // loads per wavefront and step, 1024 bytes each
   static_assert(NW % 2 == 0, "a wavefront's loads are all of even or all of odd eights of lines");
   const char* base;
   int64_t step;   // bytes from one step to the next
-  int64_t ld2;
-  int64_t left;   // KC: bytes from base to the end of the matrix's last line; else bytes of a row from base on
-  int64_t K;
+  int ld2, K;
+  int left;       // KC: bytes from base to the end of the matrix's last line; else bytes of a row from base on
   int off[J];
   int chunk8;     // KC: first k of this lane's chunk
 
-  __device__ __forceinline__ void init(const Mat& m, int64_t line0, int64_t lines, int64_t k, int wave, int lane) {
-    ld2 = m.ld * 2;
+  __device__ __forceinline__ void init(const Mat& m, int64_t line0, int64_t lines, int k, int wave, int lane) {
+    ld2 = (int)m.ld * 2;
     K = k;
     if (KC) {
       base = static_cast<const char*>(m.p) + line0 * ld2;
       step = kBK * 2;
-      const int64_t have = lines - line0 < LINES ? lines - line0 : LINES;
+      const int have = lines - line0 < LINES ? (int)(lines - line0) : LINES;
       left = (have - 1) * ld2 + k * 2;
       chunk8 = ((lane & 7) ^ ((wave & 1) * 4 + (lane >> 4))) * 8;  // (eight lines a load: r >> 1 & 7 of line r)
 #pragma unroll
-      for (int j = 0; j < J; ++j) off[j] = ((j * NW + wave) * 8 + (lane >> 3)) * (int)ld2 + chunk8 * 2;
+      for (int j = 0; j < J; ++j) off[j] = ((j * NW + wave) * 8 + (lane >> 3)) * ld2 + chunk8 * 2;
     } else {
       constexpr int CH = LINES / 8, R = 64 / CH;  // chunks per row, rows per load
       base = static_cast<const char*>(m.p) + line0 * 2;
-      step = kBK * ld2;
-      left = (lines - line0) * 2;
+      step = (int64_t)kBK * ld2;
+      left = (int)(lines - line0) * 2;
       chunk8 = 0;
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const int row = (j * NW + wave) * R + lane / CH, chunk = (lane % CH) ^ ((row & 3) << 2);
-        off[j] = chunk * 16 < left ? row * (int)ld2 + chunk * 16 : kFar;
+        off[j] = chunk * 16 < left ? row * ld2 + chunk * 16 : kFar;
       }
     }
   }
 
-  // part j of the tile of step s into lds (LINES * 128 bytes in all)
-  __device__ __forceinline__ void load(int j, int64_t s, char* lds, int wave) const {
-    const int64_t kleft = K - s * kBK;
-    int64_t limit = KC ? left - s * step : ((kleft < kBK ? kleft : kBK) - 1) * ld2 + left;
-    if (kleft <= 0) limit = 0;  // (behind the last step: zeros, which nothing reads)
-    buffer_to_lds(base + s * step, (uint32_t)limit, lds + (j * NW + wave) * 1024, !KC || chunk8 < kleft ? off[j] : kFar);
+  // The tile of step s: where it begins, and how much of what follows belongs to the matrix (behind the last step:
+  // nothing, and the loads give zeros that nothing reads).
+  struct Aim {
+    const char* from;
+    uint32_t bytes;
+    bool in;
+  };
+  __device__ __forceinline__ Aim aim(int s) const {
+    const int kleft = K - s * kBK;
+    const int n = KC ? (kleft > 0 ? left - s * (kBK * 2) : 0) : ((kleft < kBK ? kleft : kBK) - 1) * ld2 + left;
+    return {base + s * step, (uint32_t)(n > 0 && kleft > 0 ? n : 0), !KC || chunk8 < kleft};
+  }
+  // part j of it into lds (LINES * 128 bytes in all)
+  __device__ __forceinline__ void load(int j, const Aim& a, char* lds, int wave) const {
+    buffer_to_lds(a.from, a.bytes, lds + (j * NW + wave) * 1024, a.in ? off[j] : kFar);
   }
 };
 
@@ -630,11 +639,10 @@ struct StreamKept {
     uint32_t s[J];
   };
   const uint8_t *codes, *scales;
-  int64_t K;
-  int32_t row_bytes, G, left;
+  int32_t K, row_bytes, G, left;
   int off[J], soff[J], to[J];
 
-  __device__ __forceinline__ void init(const Kept& k, int64_t line0, int64_t rows, int tid) {
+  __device__ __forceinline__ void init(const Kept& k, int64_t line0, int rows, int tid) {
     row_bytes = k.G * kGroup;
     G = k.G;
     K = rows;
@@ -651,11 +659,11 @@ struct StreamKept {
     }
   }
   // the codes of a step (outside the matrix: zeros, as the scales, and 0 * 0 is what they decode to)
-  __device__ __forceinline__ void fetch(int64_t step, Codes& c) const {
-    const int64_t k0 = step * kBK, kleft = K - k0;
-    const int rows = kleft < kBK ? (int)kleft : kBK;
-    const auto rc = EF_BUFFER(codes + k0 * row_bytes, kleft > 0 ? (rows - 1) * row_bytes + left : 0);
-    const auto rs = EF_BUFFER(scales + k0 * G, kleft > 0 ? (rows - 1) * G + left / kGroup : 0);
+  __device__ __forceinline__ void fetch(int step, Codes& c) const {
+    const int kleft = K - step * kBK, rows = kleft < kBK ? kleft : kBK;
+    const int nc = (rows - 1) * row_bytes + left, ns = (rows - 1) * G + left / kGroup;  // (no rows: 0 or less)
+    const auto rc = EF_BUFFER(codes + (int64_t)step * kBK * row_bytes, nc > 0 ? nc : 0);
+    const auto rs = EF_BUFFER(scales + (int64_t)step * kBK * G, ns > 0 ? ns : 0);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       c.q[j] = EF_BUFFER_B128(rc, off[j]);
@@ -749,8 +757,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
   tile_of(blockIdx.x, ((uint32_t)M + BM - 1) / BM, ((uint32_t)N + BN - 1) / BN, &ti, &tj);
   const int64_t m0 = (int64_t)ti * BM, n0 = (int64_t)tj * BN;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * 64;
-  const int64_t all = ((int64_t)K + kBK - 1) / kBK;
-  const int64_t s0 = (int64_t)blockIdx.y * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
+  const int all = (K + kBK - 1) / kBK, s0 = (int)blockIdx.y * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
 
   Stream<AKC, BM, NW> sa;
   sa.init(A, m0, M, K, wave, lane);
@@ -771,7 +778,9 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
     for (int b = 0; b < TN; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.0f;
-  const bool sums = KIND == K_WGRAD && ep.db && n0 == 0 && wn == 0;
+  // db: the workgroups of the first column of tiles add up A's lines as they go by, each of the wavefronts that share
+  // them the slices ks = wave % WN of every step.
+  const int sum_slice = KIND == K_WGRAD && ep.db && n0 == 0 ? wave % WN : -1;
   float bs[TM];
 #pragma unroll
   for (int a = 0; a < TM; ++a) bs[a] = 0.0f;
@@ -794,10 +803,6 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
       }
       between(i);
       __builtin_amdgcn_sched_barrier(0);
-    }
-    if (sums) {
-#pragma unroll
-      for (int a = 0; a < TM; ++a) bs[a] = add8(fa[h][a], bs[a]);
     }
   };
   // Tiles of A take turns in three parts of the LDS, those of B in two.  Behind the barrier that ends step s its last
@@ -827,22 +832,26 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
       sk.put(f, w, to);
     }
   };
-  char *a0 = lds, *a1 = lds + kA, *a2 = lds + 2 * kA;
-  char* const b0 = lds + 3 * kA;
-  char* const b1 = b0 + kB;
+  char* const b0 = lds;  // (first: offsets within B's parts fit the instructions)
+  char* const b1 = lds + kB;
+  char *a0 = lds + 2 * kB, *a1 = a0 + kA, *a2 = a1 + kA;
   if (B8) {
     sk.fetch(s0, codes[0]);
     sk.fetch(s0 + 1, codes[1]);
   }
+  {
+    const auto a = sa.aim(s0), a_next = sa.aim(s0 + 1);
+    const auto b = sb.aim(s0), b_next = sb.aim(s0 + 1);
 #pragma unroll
-  for (int j = 0; j < SA::J; ++j) {
-    sa.load(j, s0, a0, wave);
-    if (!B8) sb.load(j, s0, b0, wave);
-  }
+    for (int j = 0; j < SA::J; ++j) {
+      sa.load(j, a, a0, wave);
+      if (!B8) sb.load(j, b, b0, wave);
+    }
 #pragma unroll
-  for (int j = 0; j < SA::J; ++j) {
-    sa.load(j, s0 + 1, a1, wave);
-    if (!B8) sb.load(j, s0 + 1, b1, wave);
+    for (int j = 0; j < SA::J; ++j) {
+      sa.load(j, a_next, a1, wave);
+      if (!B8) sb.load(j, b_next, b1, wave);
+    }
   }
   if (B8) {
     decode(codes[0], 0, 4, b0);
@@ -856,29 +865,40 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
 #pragma unroll
   for (int t = 0; t < TN; ++t) fb[0][t] = rb.read(b0, 0, t);
   // Step s in a0 and cur, s + 1 in a1 and nxt (of its checkpoint, in `now`, a quarter); `then` has the codes of s + 2.
-  auto advance = [&](int64_t s, char* cur, char* nxt, typename SK::Codes& now, typename SK::Codes& then) {
+  auto sum = [&](int h, int ks) {
+    if (KIND == K_WGRAD && sum_slice >= 0 && (WN == 4 ? ks == sum_slice : (ks & 1) == sum_slice)) {
 #pragma unroll
-    for (int ks = 0; ks < 3; ++ks)
+      for (int a = 0; a < TM; ++a) bs[a] = add8(fa[h][a], bs[a]);
+    }
+  };
+  auto advance = [&](int s, char* cur, char* nxt, typename SK::Codes& now, typename SK::Codes& then) {
+    const auto a = sa.aim(s + 2);
+#pragma unroll
+    for (int ks = 0; ks < 3; ++ks) {
       slice(std::true_type{}, ks & 1, a0, cur, ks + 1, [&](int i) {
         const int j = (ks * kMul + i) / kGap;
-        if (i % kGap == 0 && j < SA::J) sa.load(j, s + 2, a2, wave);
+        if (i % kGap == 0 && j < SA::J) sa.load(j, a, a2, wave);
         if (B8) quarter(i, now, ks + 1, nxt);
       });
+      sum(ks & 1, ks);
+    }
     // This wavefront's part of the next step has arrived (all but the last loads, of A behind it), and its last reads
     // of this one.
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SA::J) : "memory");
+    const auto b = sb.aim(s + 2);
     slice(std::true_type{}, 1, a1, nxt, 0, [&](int i) {
       if (B8 && i == 0) sk.fetch(s + 3, now);
-      if (!B8 && i % kGap == 0 && i / kGap < SB::J) sb.load(i / kGap, s + 2, cur, wave);
+      if (!B8 && i % kGap == 0 && i / kGap < SB::J) sb.load(i / kGap, b, cur, wave);
       if (B8) quarter(i, then, 0, cur);
     });
+    sum(1, 3);
     char* x = a0;
     a0 = a1;
     a1 = a2;
     a2 = x;
   };
   static_assert(SA::J == SB::J && kMul / kGap >= SB::J, "B's loads fit a slice");
-  int64_t s = s0;
+  int s = s0;
   for (; s + 2 < s1; s += 2) {
     advance(s, b0, b1, codes[1], codes[0]);
     advance(s + 1, b1, b0, codes[0], codes[1]);
@@ -889,13 +909,30 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
     last = b1;
   }
 #pragma unroll
-  for (int ks = 0; ks < 3; ++ks) slice(std::true_type{}, ks & 1, a0, last, ks + 1, [](int) {});
+  for (int ks = 0; ks < 3; ++ks) {
+    slice(std::true_type{}, ks & 1, a0, last, ks + 1, [](int) {});
+    sum(ks & 1, ks);
+  }
   slice(std::false_type{}, 1, a0, last, 0, [](int) {});
+  sum(1, 3);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   static_assert(slab_bytes(NW, 2) <= sizeof(lds), "the epilogue's part of the LDS");
+  if (KIND == K_WGRAD && ep.db && n0 == 0) {  // the wavefronts' sums of a line, in order
+    float* share = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int a = 0; a < TM; ++a) share[(wave * TM + a) * 64 + lane] = bs[a];
+    __syncthreads();
+    if (wn == 0) {
+#pragma unroll
+      for (int a = 0; a < TM; ++a)
+#pragma unroll
+        for (int z = 1; z < WN; ++z) bs[a] += share[((wave + z) * TM + a) * 64 + lane];
+      finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
+    }
+    __syncthreads();
+  }
   finish<KIND, DO, TM, 2>(acc, lds, wave, lane, m0 + wm, n0 + wn, M, N, ep, sp);
-  if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -82,7 +82,7 @@ bool fast_mat(const Mat& m, int64_t cols) {
 
 template <int KIND>
 bool fast_ok(const Product& p) {
-  if (p.K == 0 || !fast_mat(p.A, KIND == K_WGRAD ? p.M : p.K)) return false;
+  if (p.K == 0 || p.K > ((int64_t)1 << 30) || !fast_mat(p.A, KIND == K_WGRAD ? p.M : p.K)) return false;
   return KIND == K_WGRAD ? p.N <= kFastLd : fast_mat(p.B, KIND == K_FWD ? p.K : p.N);
 }
 

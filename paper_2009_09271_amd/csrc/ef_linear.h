@@ -71,7 +71,14 @@ __device__ __forceinline__ void load8(const void* p, int64_t at, int cnt, float 
   }
 }
 
-template <int DT>
+// ONCE: past the caches
+template <bool ONCE>
+__device__ __forceinline__ void store16(u32x4 a, void* p) {
+  if (ONCE) __builtin_nontemporal_store(a, static_cast<u32x4u*>(p));
+  else *static_cast<u32x4u*>(p) = a;
+}
+
+template <int DT, bool ONCE = false>
 __device__ __forceinline__ void store8(void* p, int64_t at, int cnt, const float (&v)[8]) {
   if (DT == EF_F32) {
     float* q = static_cast<float*>(p) + at;
@@ -82,8 +89,8 @@ __device__ __forceinline__ void store8(void* p, int64_t at, int cnt, const float
         a[j] = __float_as_uint(v[j]);
         b[j] = __float_as_uint(v[j + 4]);
       }
-      *reinterpret_cast<u32x4u*>(q) = a;
-      *reinterpret_cast<u32x4u*>(q + 4) = b;
+      store16<ONCE>(a, q);
+      store16<ONCE>(b, q + 4);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -95,7 +102,7 @@ __device__ __forceinline__ void store8(void* p, int64_t at, int cnt, const float
 #pragma unroll
     for (int j = 0; j < 4; ++j) a[j] = f_bf16x2(v[2 * j], v[2 * j + 1]);
     if (cnt >= 8) {
-      *reinterpret_cast<u32x4u*>(q) = a;
+      store16<ONCE>(a, q);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -103,6 +110,34 @@ __device__ __forceinline__ void store8(void* p, int64_t at, int cnt, const float
     }
   }
 }
+
+// Eight neighbours of a row as they are stored, for loads that are used later.
+template <int DT>
+struct Raw {
+  static constexpr int W = DT == EF_F32 ? 8 : 4;
+  uint32_t r[W];
+
+  // ONCE: past the caches
+  template <bool ONCE = false>
+  __device__ __forceinline__ void load(const void* p, int64_t at, int cnt) {
+    if (cnt >= 8) {
+      const u32x4u* from = reinterpret_cast<const u32x4u*>(static_cast<const char*>(p) + at * (W / 2));
+#pragma unroll
+      for (int j = 0; j < W / 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[4 * j + i] = (ONCE ? __builtin_nontemporal_load(from + j) : from[j])[i];
+    } else {
+      float v[8];
+      load8<DT>(p, at, cnt, v);
+#pragma unroll
+      for (int j = 0; j < W; ++j) r[j] = DT == EF_F32 ? __float_as_uint(v[j]) : f_bf16x2(v[2 * j % 8], v[(2 * j + 1) % 8]);
+    }
+  }
+  __device__ __forceinline__ float value(int j) const {
+    if (DT == EF_F32) return __uint_as_float(r[j % W]);
+    return __uint_as_float(j & 1 ? r[j / 2 % W] & 0xFFFF0000u : r[j / 2 % W] << 16);
+  }
+};
 
 // ---------------------------------------------------------------------------------------------
 // Codes.
@@ -142,14 +177,28 @@ __device__ __forceinline__ u32x2 encode8(const float (&v)[8], uint32_t s, int fm
   return q;
 }
 
+// The signed bytes 2 HI and 2 HI + 1 of w as floats.  (Written out: from the conversion itself the compiler keeps a whole
+// step's bytes of the weight gradient apart, and spills.)
+template <int HI>
+__device__ __forceinline__ void bytes(uint32_t w, float* a, float* b) {
+  if (HI) {
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(*a) : "v"(w));
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(*b) : "v"(w));
+  } else {
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(*a) : "v"(w));
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(*b) : "v"(w));
+  }
+}
+
 __device__ __forceinline__ void decode8(u32x2 q, uint32_t s, int fmt, float (&v)[8]) {
   const float r = __uint_as_float(s << 23);  // 2^e; scale byte 255: infinity, and 0 * infinity is NaN
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     if (fmt == EF_CKPT_INT8) {
-      const uint32_t w = q[h] ^ 0x80808080u;  // code + 128, a byte that converts by itself
+      bytes<0>(q[h], &v[4 * h], &v[4 * h + 1]);
+      bytes<1>(q[h], &v[4 * h + 2], &v[4 * h + 3]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[4 * h + j] = ((float)(w >> (8 * j) & 255u) - 128.0f) * r;
+      for (int j = 0; j < 4; ++j) v[4 * h + j] *= r;
     } else {
       const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[h], false);
       const auto b = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[h], true);
@@ -228,10 +277,7 @@ __device__ __forceinline__ void act_value(float (&v)[8], int act) {
   }
 }
 
-// v *= the derivative at z.  Far out, where it is 0 or 1 to float32, z is held at a bound: no product there
-// overflows.  (The logistic function at -u is taken by itself: 1 minus that at u would cancel.)
-__device__ __forceinline__ float held(float z, float b) { return z > b ? b : (z < -b ? -b : z); }
-
+// v *= the derivative at z.  (The logistic function at -u is taken by itself: 1 minus that at u would cancel.)
 __device__ __forceinline__ void act_slope(float (&v)[8], const float (&z)[8], int act) {
   switch (act) {
     case EF_ACT_RELU:
@@ -241,24 +287,24 @@ __device__ __forceinline__ void act_slope(float (&v)[8], const float (&z)[8], in
     case EF_ACT_GELU:
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float x = held(z[j], 16.0f);
         float d;
-        const float p = normal_cdf(x, &d);
-        v[j] *= fmaf(x, d, p);
+        const float p = normal_cdf(z[j], &d);
+        v[j] *= fmaf(z[j], d, p);
       }
       break;
     case EF_ACT_GELU_TANH:
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float x = held(z[j], 16.0f), t = gelu_t(x), p = logistic2(t), q = logistic2(-t);
-        v[j] *= fmaf(x * p * q, 2.0f * kGeluA * fmaf(3.0f * kGeluB * x, x, 1.0f), p);
+        // (held where the derivative is 0 or 1 to float32: the square of a larger z could overflow; a NaN comes back in)
+        const float x = __builtin_amdgcn_fmed3f(z[j], -16.0f, 16.0f), t = gelu_t(x), p = logistic2(t), q = logistic2(-t);
+        v[j] *= fmaf(x * p * q, 2.0f * kGeluA * fmaf(3.0f * kGeluB * x, x, 1.0f), fmaf(z[j], 0.0f, p));
       }
       break;
     case EF_ACT_SILU:
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float x = held(z[j], 128.0f), p = logistic2(-kLog2e * x), q = logistic2(kLog2e * x);
-        v[j] *= fmaf(x * p, q, p);
+        const float p = logistic2(-kLog2e * z[j]), q = logistic2(kLog2e * z[j]);
+        v[j] *= fmaf(z[j] * p, q, p);
       }
       break;
   }
@@ -275,45 +321,45 @@ struct Kept {
   int32_t fmt;
 };
 
+// What is read once and by nobody else goes past the caches (16384 x 4096 in bfloat16: pack 42 -> 34 us, unpack 34 -> 31;
+// two or four rows a lane: 46 and 49 us); so does what act_backward writes (67 -> 65).
 template <int DT>
 __global__ __launch_bounds__(256) void k_ckpt_pack(int64_t n, int32_t c, const void* x, int64_t ldx, Kept k, int txs) {
   const int tx = threadIdx.x & ((1 << txs) - 1), ty = threadIdx.x >> txs;
   const int64_t row = (int64_t)blockIdx.x * (256 >> txs) + ty;
   const int32_t col = ((int32_t)(blockIdx.y << txs) + tx) * 8;
   if (row >= n || col >= k.G * kGroup) return;  // (whole groups: 4 lanes, 32 columns)
+  Raw<DT> raw;
+  raw.template load<true>(x, row * ldx + col, c - col);
   float v[8];
-  load8<DT>(x, row * ldx + col, c - col, v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = raw.value(j);
   const uint32_t s = group_scale(group_amax(v), k.fmt);
-  *reinterpret_cast<u32x2u*>(k.codes + row * k.G * kGroup + col) = encode8(v, s, k.fmt);
+  *reinterpret_cast<u32x2*>(k.codes + row * k.G * kGroup + col) = encode8(v, s, k.fmt);
   if ((col & (kGroup - 1)) == 0) k.scales[row * k.G + col / kGroup] = (uint8_t)s;
 }
 
-template <int DT>
-__global__ __launch_bounds__(256) void k_ckpt_unpack(int64_t n, int32_t c, Kept k, void* y, int64_t ldy, int txs) {
+// ACT: y = dy * act'(x^), rounded once (y may be dy); else y = x^.
+template <int DT, bool ACT>
+__global__ __launch_bounds__(256) void k_ckpt_unpack(int64_t n, int32_t c, int act, Kept k, const void* dy, int64_t lddy, void* y,
+                                                     int64_t ldy, int txs) {
   const int tx = threadIdx.x & ((1 << txs) - 1), ty = threadIdx.x >> txs;
   const int64_t row = (int64_t)blockIdx.x * (256 >> txs) + ty;
   const int32_t col = ((int32_t)(blockIdx.y << txs) + tx) * 8;
   if (row >= n || col >= c) return;
-  float v[8];
-  decode8(*reinterpret_cast<const u32x2u*>(k.codes + row * k.G * kGroup + col), k.scales[row * k.G + col / kGroup],
-          k.fmt, v);
-  store8<DT>(y, row * ldy + col, c - col, v);
-}
-
-// dz = dy * act'(x^), rounded once.
-template <int DT>
-__global__ __launch_bounds__(256) void k_ckpt_act_backward(int64_t n, int32_t c, int act, Kept k, const void* dy,
-                                                           int64_t lddy, void* dz, int64_t lddz, int txs) {
-  const int tx = threadIdx.x & ((1 << txs) - 1), ty = threadIdx.x >> txs;
-  const int64_t row = (int64_t)blockIdx.x * (256 >> txs) + ty;
-  const int32_t col = ((int32_t)(blockIdx.y << txs) + tx) * 8;
-  if (row >= n || col >= c) return;
+  const u32x2* from = reinterpret_cast<const u32x2*>(k.codes + row * k.G * kGroup + col);
+  const u32x2 q = ACT ? *from : __builtin_nontemporal_load(from);
+  const uint32_t s = k.scales[row * k.G + col / kGroup];
   float v[8], z[8];
-  load8<DT>(dy, row * lddy + col, c - col, v);
-  decode8(*reinterpret_cast<const u32x2u*>(k.codes + row * k.G * kGroup + col), k.scales[row * k.G + col / kGroup],
-          k.fmt, z);
-  act_slope(v, z, act);
-  store8<DT>(dz, row * lddz + col, c - col, v);
+  Raw<DT> raw;
+  if (ACT) raw.load(dy, row * lddy + col, c - col);
+  decode8(q, s, k.fmt, z);
+  if (ACT) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = raw.value(j);
+    act_slope(v, z, act);
+  }
+  store8<DT, ACT>(y, row * ldy + col, c - col, ACT ? v : z);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -331,32 +377,6 @@ struct Epi {
   int32_t act;
   int32_t add;        // wgrad: dw += product, db += sum
   void* db;           // wgrad: [M], the sums of A's lines, or null
-};
-
-// Eight neighbours of a row as they are stored, for loads that are used later.
-template <int DT>
-struct Raw {
-  static constexpr int W = DT == EF_F32 ? 8 : 4;
-  uint32_t r[W];
-
-  __device__ __forceinline__ void load(const void* p, int64_t at, int cnt) {
-    if (cnt >= 8) {
-      const u32x4u* from = reinterpret_cast<const u32x4u*>(static_cast<const char*>(p) + at * (W / 2));
-#pragma unroll
-      for (int j = 0; j < W / 4; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[4 * j + i] = from[j][i];
-    } else {
-      float v[8];
-      load8<DT>(p, at, cnt, v);
-#pragma unroll
-      for (int j = 0; j < W; ++j) r[j] = DT == EF_F32 ? __float_as_uint(v[j]) : f_bf16x2(v[2 * j % 8], v[(2 * j + 1) % 8]);
-    }
-  }
-  __device__ __forceinline__ float value(int j) const {
-    if (DT == EF_F32) return __uint_as_float(r[j % W]);
-    return __uint_as_float(j & 1 ? r[j / 2 % W] & 0xFFFF0000u : r[j / 2 % W] << 16);
-  }
 };
 
 // What the epilogue reads beside C for eight columns of a row, loaded ahead of its use; KIND the product, DT the type
@@ -668,18 +688,6 @@ struct StreamKept {
     for (int j = 0; j < J; ++j) {
       c.q[j] = EF_BUFFER_B128(rc, off[j]);
       c.s[j] = EF_BUFFER_B8(rs, soff[j]);
-    }
-  }
-  // the signed byte 2 * HI or 2 * HI + 1 of w as a float (written out: the compiler, given the conversion, keeps the
-  // bytes of a whole step apart and spills)
-  template <int HI>
-  static __device__ __forceinline__ void bytes(uint32_t w, float* a, float* b) {
-    if (HI) {
-      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(*a) : "v"(w));
-      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(*b) : "v"(w));
-    } else {
-      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(*a) : "v"(w));
-      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(*b) : "v"(w));
     }
   }
   // codes 2 h and 2 h + 1 of quarter f

@@ -234,8 +234,10 @@ int ef_ckpt_unpack(int64_t n, int64_t c, const uint8_t* codes, const uint8_t* sc
   Flat f;
   EF_TRY(flat_of(n, c, &f));
   const Kept k{const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), groups(c), fmt};
-  if (dtype == EF_F32) EF_LAUNCH(k_ckpt_unpack<EF_F32>, f.grid, dim3(256), 0, S(stream), n, (int32_t)c, k, y, ldy, f.txs);
-  else EF_LAUNCH(k_ckpt_unpack<EF_BF16>, f.grid, dim3(256), 0, S(stream), n, (int32_t)c, k, y, ldy, f.txs);
+  if (dtype == EF_F32)
+    EF_LAUNCH((k_ckpt_unpack<EF_F32, false>), f.grid, dim3(256), 0, S(stream), n, (int32_t)c, 0, k, nullptr, (int64_t)0, y, ldy, f.txs);
+  else
+    EF_LAUNCH((k_ckpt_unpack<EF_BF16, false>), f.grid, dim3(256), 0, S(stream), n, (int32_t)c, 0, k, nullptr, (int64_t)0, y, ldy, f.txs);
   return launched();
 }
 
@@ -253,9 +255,9 @@ int ef_ckpt_act_backward(int64_t n, int64_t c, int act, const uint8_t* codes, co
   EF_TRY(flat_of(n, c, &f));
   const Kept k{const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), groups(c), fmt};
   if (dtype == EF_F32)
-    EF_LAUNCH(k_ckpt_act_backward<EF_F32>, f.grid, dim3(256), 0, S(stream), n, (int32_t)c, act, k, dy, lddy, dz, lddz, f.txs);
+    EF_LAUNCH((k_ckpt_unpack<EF_F32, true>), f.grid, dim3(256), 0, S(stream), n, (int32_t)c, act, k, dy, lddy, dz, lddz, f.txs);
   else
-    EF_LAUNCH(k_ckpt_act_backward<EF_BF16>, f.grid, dim3(256), 0, S(stream), n, (int32_t)c, act, k, dy, lddy, dz, lddz, f.txs);
+    EF_LAUNCH((k_ckpt_unpack<EF_BF16, true>), f.grid, dim3(256), 0, S(stream), n, (int32_t)c, act, k, dy, lddy, dz, lddz, f.txs);
   return launched();
 }
 

@@ -944,7 +944,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
 }
 
 // ---------------------------------------------------------------------------------------------
-// The same products for every type and alignment.  Operands pass through registers, a step of 32 ahead.  A float32
+// The same products for every type and alignment.  Operands pass through registers, two steps of 32 ahead.  A float32
 // value goes into the LDS as three bfloat16 numbers, hi + mid + lo: rounded to nearest three times, which leaves
 // nothing of its 24 bits.  Of the nine products of two such sums the six that matter are taken; what is left out is
 // 2^-23 of the product at most.  A checkpoint's values are bfloat16 numbers, so against them three products are the
@@ -1040,9 +1040,9 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
   tile_of(blockIdx.x, ((uint32_t)M + kAnyTile - 1) / kAnyTile, ((uint32_t)N + kAnyTile - 1) / kAnyTile, &ti, &tj);
   const int64_t m0 = (int64_t)ti * kAnyTile, n0 = (int64_t)tj * kAnyTile;
   const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-  Chunks<DT, AKC, PA> ca;
-  Chunks<DT, BKC, PB> cb;
-  KeptChunks ck;
+  Chunks<DT, AKC, PA> ca[2];
+  Chunks<DT, BKC, PB> cb[2];
+  KeptChunks ck[2];
   Reader<AKC, kAnyTile, 2, kAnyK> ra;
   Reader<BKC, kAnyTile, 2, kAnyK> rb;
   ra.init(wm, lane);
@@ -1058,19 +1058,18 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
   float bs[2] = {0.0f, 0.0f};
   const int64_t all = ((int64_t)K + kAnyK - 1) / kAnyK;
   const int64_t s0 = (int64_t)blockIdx.y * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
-  auto fetch = [&](int64_t s) {
-    ca.fetch(A, m0, M, s * kAnyK, K, t);
-    if (B8) ck.fetch(BK, n0, N, s * kAnyK, K, t);
-    else cb.fetch(B, n0, N, s * kAnyK, K, t);
+  auto fetch = [&](int64_t s, int set) {
+    ca[set].fetch(A, m0, M, s * kAnyK, K, t);
+    if (B8) ck[set].fetch(BK, n0, N, s * kAnyK, K, t);
+    else cb[set].fetch(B, n0, N, s * kAnyK, K, t);
   };
-  if (s0 < s1) fetch(s0);
-  for (int64_t s = s0; s < s1; ++s) {
+  auto step = [&](int64_t s, int set) {
     __syncthreads();
-    ca.put(lds, t);
-    if (B8) ck.put(lds + PA * kPlane, BK.fmt, t);
-    else cb.put(lds + PA * kPlane, t);
+    ca[set].put(lds, t);
+    if (B8) ck[set].put(lds + PA * kPlane, BK.fmt, t);
+    else cb[set].put(lds + PA * kPlane, t);
     __syncthreads();
-    if (s + 1 < s1) fetch(s + 1);
+    if (s + 2 < s1) fetch(s + 2, set);
 #pragma unroll
     for (int ks = 0; ks < kAnyK / 16; ++ks) {
       bf16x8 fa[PA][2], fb[PB][2];
@@ -1099,6 +1098,12 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
           for (int a = 0; a < 2; ++a) bs[a] = add8(fa[p][a], bs[a]);
       }
     }
+  };
+  if (s0 < s1) fetch(s0, 0);
+  if (s0 + 1 < s1) fetch(s0 + 1, 1);
+  for (int64_t s = s0; s < s1; s += 2) {
+    step(s, 0);
+    if (s + 1 < s1) step(s + 1, 1);
   }
   __syncthreads();
   finish<KIND, DO, 2, 1>(acc, lds, wave, lane, m0 + wm, n0 + wn, M, N, ep, sp);

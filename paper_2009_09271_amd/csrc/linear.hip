@@ -95,36 +95,44 @@ struct Plan {
 
 constexpr int kCUs = 256;
 
-// Microseconds that a form takes, from what was measured: `step` for one step along k of the workgroups that a CU
-// holds (one of 256 x 256 or of k_linear_any; two of 128 x 128, `half` where it holds one), `fixed` for its start
-// and its epilogue; joining: a launch, and the partial sums written and read.
+// Microseconds that a form takes, fitted to what was measured: for each round of the workgroups that the CUs hold at
+// one time, `few` to `full` for one step along k (from where half of them are at work, one a CU, to all of them:
+// workgroups share a CU, and the chip its power) and `fixed` for the start and the epilogue; then the partial sums
+// written, and the join: a launch, and the sums read.  For instance forward, n, i, o = 2048, 4096, 4096: 128 x 128 tiles
+// 67 measured, 67 by this; 256 x 256 tiles 84 and 82, in two parts of k 79 and 90.  8192, 4096, 4096: 256 x 256 tiles 238
+// and 236.  wgrad of 8192 tokens, 768 x 768, 128 x 128 tiles, in 4, 7 and 14 parts: 34, 28 and 29; 41, 29 and 29.
 struct Cost {
   int tile, k, per_cu;
-  double step, half, fixed;
+  double few, full, fixed;
 };
-constexpr Cost kCosts[3] = {{kAnyTile, kAnyK, 2, 1.4, 1.0, 4.0}, {128, kBK, 2, 0.75, 0.45, 4.0}, {256, kBK, 1, 1.3, 1.3, 6.0}};
+Cost cost_of_form(int form, bool wgrad, bool f32) {
+  if (form == kLarge) return {256, kBK, 1, 1.1, wgrad ? 1.8 : 1.7, wgrad ? 17.0 : 10.0};
+  if (form == kSmall) return {128, kBK, 2, wgrad ? 0.9 : 0.45, wgrad ? 1.3 : 0.95, 6.0};
+  return {kAnyTile, kAnyK, 2, f32 && !wgrad ? 2.3 : 1.5, f32 && !wgrad ? 3.3 : 2.1, 5.0};
+}
 
-double cost_of(const Cost& c, int64_t M, int64_t N, int64_t K, int64_t splits, int64_t per) {
+double cost_of(const Cost& c, int64_t M, int64_t N, int64_t splits, int64_t per) {
   const double wgs = (double)((M + c.tile - 1) / c.tile) * (double)((N + c.tile - 1) / c.tile) * (double)splits;
-  const double rounds = std::ceil(wgs / (kCUs * c.per_cu));
-  double t = rounds * ((wgs <= kCUs ? c.half : c.step) * (double)per + c.fixed);
-  if (splits > 1) t += 4.0 + (double)splits * (double)M * (double)N * 8.0 / 4.5e6;
+  const double slots = (double)kCUs * c.per_cu, rounds = std::ceil(wgs / slots);
+  const double busy = std::min(std::max(2.0 * wgs / slots - 1.0, 0.0), 1.0);
+  double t = rounds * ((c.few + (c.full - c.few) * busy) * (double)per + c.fixed);
+  if (splits > 1) t += 3.5 + (double)splits * (double)M * (double)N * (4.0 / 6e6 + 4.0 / 5e6);
   return t;
 }
 
-// The form and the number of splits that these costs are least for.  The choice goes by sizes and alignment alone:
-// the same call always sums in the same order.
-Plan plan_of(bool fast, int64_t M, int64_t N, int64_t K) {
+// The form and the number of splits that these costs are least for.  The choice goes by sizes, types and alignment
+// alone: the same call always sums in the same order.
+Plan plan_of(bool fast, bool wgrad, bool f32, int64_t M, int64_t N, int64_t K) {
   Plan best{kAny, 1, 1};
   double least = 0.0;
   for (int f = fast ? kSmall : kAny; f <= (fast ? kLarge : kAny); ++f) {
-    const Cost& c = kCosts[f];
+    const Cost c = cost_of_form(f, wgrad, f32);
     const int64_t steps = std::max<int64_t>((K + c.k - 1) / c.k, 1);
     const int64_t tiles = ((M + c.tile - 1) / c.tile) * ((N + c.tile - 1) / c.tile);
     for (int64_t s = 1; s <= 64 && s <= steps && (s == 1 || tiles * s <= 2 * kCUs * c.per_cu); ++s) {
       const int64_t per = (steps + s - 1) / s, splits = (steps + per - 1) / per;
       if (splits != s) continue;
-      const double t = cost_of(c, M, N, K, splits, per);
+      const double t = cost_of(c, M, N, splits, per);
       if (least == 0.0 || t < least) {
         least = t;
         best = {(Form)f, (int32_t)splits, (int32_t)per};
@@ -137,15 +145,15 @@ Plan plan_of(bool fast, int64_t M, int64_t N, int64_t K) {
 int32_t padded(int64_t N) { return groups(N) * kGroup; }
 
 // The workspace of a product, whatever the alignment of its matrices turns out to be.
-size_t product_bytes(int dtype, int64_t M, int64_t N, int64_t K) {
-  int32_t splits = M ? plan_of(false, M, N, K).splits : 1;
-  if (M && dtype == EF_BF16) splits = std::max(splits, plan_of(true, M, N, K).splits);
+size_t product_bytes(bool wgrad, int dtype, int64_t M, int64_t N, int64_t K) {
+  int32_t splits = M ? plan_of(false, wgrad, dtype == EF_F32, M, N, K).splits : 1;
+  if (M && dtype == EF_BF16) splits = std::max(splits, plan_of(true, wgrad, false, M, N, K).splits);
   return splits == 1 ? 0 : align_up((size_t)splits * ((size_t)M * padded(N) + (size_t)M) * 4, kAlign);
 }
 
 template <int KIND, int DT, int DO>
 int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
-  const size_t need = product_bytes(DT, p.M, p.N, p.K);
+  const size_t need = product_bytes(KIND == K_WGRAD, DT, p.M, p.N, p.K);
   if (need) {
     if (!ws || !aligned(ws, kAlign)) return EF_EINVAL;
     if (ws_bytes < need) return EF_EWORKSPACE;
@@ -165,9 +173,8 @@ int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
       return launched();
     }
   }
-  const Plan pl = plan_of(fast, p.M, p.N, p.K);
-  const Cost& c = kCosts[pl.form];
-  const int64_t tiles = ((p.M + c.tile - 1) / c.tile) * ((p.N + c.tile - 1) / c.tile);
+  const Plan pl = plan_of(fast, KIND == K_WGRAD, DT == EF_F32, p.M, p.N, p.K);
+  const int64_t tile = pl.form == kLarge ? 256 : 128, tiles = ((p.M + tile - 1) / tile) * ((p.N + tile - 1) / tile);
   if (tiles > kMaxGrid) return EF_ERANGE;
   Split sp{nullptr, nullptr, p.M * padded(p.N), padded(p.N), pl.per};
   if (pl.splits > 1) {
@@ -264,7 +271,7 @@ int ef_ckpt_act_backward(int64_t n, int64_t c, int act, const uint8_t* codes, co
 size_t ef_linear_workspace_bytes(int op, int64_t n, int64_t i, int64_t o, int dtype) {
   if (check_sizes(n, i, o) != EF_OK || !dtype_ok(dtype) || op < EF_OP_FORWARD || op > EF_OP_WGRAD) return 0;
   const int64_t M = op == EF_OP_WGRAD ? o : n, N = op == EF_OP_FORWARD ? o : i, K = op == EF_OP_FORWARD ? i : op == EF_OP_DGRAD ? o : n;
-  return product_bytes(dtype, M, N, K);
+  return product_bytes(op == EF_OP_WGRAD, dtype, M, N, K);
 }
 
 int ef_linear_forward(int64_t n, int64_t i, int64_t o, const void* x, int64_t ldx, const void* w, int64_t ldw,

@@ -949,41 +949,79 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
 // nothing of its 24 bits.  Of the nine products of two such sums the six that matter are taken; what is left out is
 // 2^-23 of the product at most.  A checkpoint's values are bfloat16 numbers, so against them three products are the
 // whole.  (Against the matrix instructions for float32, a sixteenth as fast: n, i, o = 1021, 771, 1285, dgrad
-// 49 -> ANY_D us; 2043, 1285, 771, wgrad 87 -> ANY_W us.)  An infinity has no such parts: it comes out as NaN.
+// 49 -> 34 us; 2043, 1285, 771, wgrad 87 -> 36 us, each with its join.)  An infinity has no such parts: it comes out as NaN.
 // A workgroup has 128 x 128 of C, four wavefronts of 64 x 64.
 // ---------------------------------------------------------------------------------------------
 constexpr int kAnyTile = 128, kAnyK = 32;
 constexpr int kPlane = kAnyTile * kAnyK * 2;
 
-// One operand's chunks of eight elements of a step, two a thread: lines by k where KC, else k by lines.
-template <int DT, bool KC, int P>
-struct Chunks {
-  Raw<DT> raw[2];
+// Where a thread's two chunks of eight elements of a step lie: eight k of a line where KC, else eight lines of a k.
+template <bool KC>
+struct Places {
   __device__ __forceinline__ static int line(int t, int j) { return KC ? (j * 256 + t) / 4 : (t & 15) * 8; }
   __device__ __forceinline__ static int k(int t, int j) { return KC ? (t & 3) * 8 : (j * 256 + t) / 16; }
-  __device__ __forceinline__ static int place(int t, int j) {
+  __device__ __forceinline__ static int lds(int t, int j) {
     const int l = line(t, j), r = k(t, j);
     return KC ? l * kAnyK * 2 + (((t & 3) ^ ((l >> 2) & 3)) << 4) : r * kAnyTile * 2 + (((t >> 2 & 3) ^ (r & 3)) << 6) + (t & 3) * 16;
   }
-  __device__ __forceinline__ void fetch(const Mat& m, int64_t line0, int64_t lines, int64_t k0, int64_t K, int t) {
+};
+
+// One operand: its chunks in registers, P bfloat16 numbers a value in the LDS.  Lines behind the last one are not
+// kept out: they repeat the last line, or line 0, or are what follows the row in memory (up to seven elements, so not
+// in the last step, whose last row may end the matrix), and reach only rows and columns of C that nobody stores.
+// Taken one by one, the last lines' elements made the workgroups at the edge wait for memory in each step (dgrad of
+// 1021, 771, 1285 in bfloat16, unsplit: 63 -> 28 us).
+template <int DT, bool KC, int P>
+struct Chunks {
+  using At = Places<KC>;
+  const char* p[2];  // this thread's chunks of the next step
+  int64_t step;      // bytes from one step to the next
+  int64_t ld;
+  int cnt;           // !KC: lines that the chunks have
+  bool narrow;       // !KC: rows of under eight elements
+  Raw<DT> raw[2][2];
+
+  __device__ __forceinline__ void init(const Mat& m, int64_t line0, int64_t lines, int64_t k0, int t) {
+    constexpr int S = DT == EF_F32 ? 4 : 2;
+    ld = m.ld * S;
+    narrow = !KC && m.ld < 8;
+    step = KC ? kAnyK * S : kAnyK * ld;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int64_t l = line0 + line(t, j), r = k0 + k(t, j);
-      const int64_t row = KC ? l : r, rows = KC ? lines : K, col = KC ? r : l, left = (KC ? K : lines) - col;
-      raw[j].load(m.p, row * m.ld + col, row < rows ? (int)(left < 8 ? left : 8) : 0);
+      int64_t l = line0 + At::line(t, j);
+      const int64_t k = k0 + At::k(t, j);
+      cnt = lines - l < 8 ? (int)(lines - l) : 8;
+      if (KC && l >= lines) l = lines - 1;
+      if (!KC && cnt <= 0) {
+        l = 0;
+        cnt = lines < 8 ? (int)lines : 8;
+      }
+      p[j] = static_cast<const char*>(m.p) + (KC ? l * ld + k * S : k * ld + l * S);
     }
   }
-  __device__ __forceinline__ void put(char* lds, int t) const {
+  // left: k from this step's first on
+  __device__ __forceinline__ void fetch(int set, int64_t left, int t) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      char* to = lds + place(t, j);
+      const int64_t mine = left - At::k(t, j);
+      int n = 8;
+      if (left <= kAnyK || narrow) n = KC ? (mine < 8 ? (int)mine : 8) : (mine > 0 ? cnt : 0);
+      raw[set][j].load(p[j], 0, n);
+      p[j] += step;
+    }
+  }
+  __device__ __forceinline__ void put(int set, char* lds, int t) const {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const Raw<DT>& r = raw[set][j];
+      char* to = lds + At::lds(t, j);
       if (P == 1) {
-        *reinterpret_cast<u32x4*>(to) = u32x4{raw[j].r[0], raw[j].r[1], raw[j].r[2], raw[j].r[3]};
+        *reinterpret_cast<u32x4*>(to) = u32x4{r.r[0], r.r[1], r.r[2], r.r[3]};
       } else {
         u32x4 w[3];
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-          float x = raw[j].value(2 * h), y = raw[j].value(2 * h + 1);
+          float x = r.value(2 * h), y = r.value(2 * h + 1);
 #pragma unroll
           for (int p = 0; p < 3; ++p) {
             // (hi is held at the largest bfloat16: a finite value does not round to an infinity, and what is not
@@ -1001,30 +1039,46 @@ struct Chunks {
 };
 
 struct KeptChunks {
-  u32x2 q[2];
-  uint32_t s[2];
-  using At = Chunks<EF_BF16, false, 1>;
-  __device__ __forceinline__ void fetch(const Kept& m, int64_t line0, int64_t lines, int64_t k0, int64_t K, int t) {
+  using At = Places<false>;
+  const uint8_t *q[2], *s[2];
+  int64_t qstep, sstep;
+  u32x2 code[2][2];
+  uint32_t scale[2][2];
+
+  __device__ __forceinline__ void init(const Kept& m, int64_t line0, int64_t k0, int t) {
+    const int64_t row = (int64_t)m.G * kGroup;
+    qstep = kAnyK * row;
+    sstep = kAnyK * (int64_t)m.G;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int64_t l = line0 + At::line(t, j), r = k0 + At::k(t, j);
-      q[j] = u32x2{0u, 0u};
-      s[j] = 0u;
-      if (r < K && l < lines) {
-        q[j] = *reinterpret_cast<const u32x2*>(m.codes + r * m.G * kGroup + l);
-        s[j] = m.scales[r * m.G + l / kGroup];
-      }
+      int64_t l = line0 + At::line(t, j);
+      if (l >= row) l = 0;
+      q[j] = m.codes + (k0 + At::k(t, j)) * row + l;
+      s[j] = m.scales + (k0 + At::k(t, j)) * m.G + l / kGroup;
     }
   }
-  __device__ __forceinline__ void put(char* lds, int fmt, int t) const {
+  __device__ __forceinline__ void fetch(int set, int64_t left, int t) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      code[set][j] = u32x2{0u, 0u};
+      scale[set][j] = 0u;
+      if (left >= kAnyK || At::k(t, j) < left) {
+        code[set][j] = *reinterpret_cast<const u32x2*>(q[j]);
+        scale[set][j] = *s[j];
+      }
+      q[j] += qstep;
+      s[j] += sstep;
+    }
+  }
+  __device__ __forceinline__ void put(int set, char* lds, int fmt, int t) const {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       float v[8];
-      decode8(q[j], s[j], fmt, v);
+      decode8(code[set][j], scale[set][j], fmt, v);
       u32x4 w;
 #pragma unroll
       for (int h = 0; h < 4; ++h) w[h] = __builtin_amdgcn_perm(__float_as_uint(v[2 * h + 1]), __float_as_uint(v[2 * h]), 0x07060302u);
-      *reinterpret_cast<u32x4*>(lds + At::place(t, j)) = w;
+      *reinterpret_cast<u32x4*>(lds + At::lds(t, j)) = w;
     }
   }
 };
@@ -1040,9 +1094,9 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
   tile_of(blockIdx.x, ((uint32_t)M + kAnyTile - 1) / kAnyTile, ((uint32_t)N + kAnyTile - 1) / kAnyTile, &ti, &tj);
   const int64_t m0 = (int64_t)ti * kAnyTile, n0 = (int64_t)tj * kAnyTile;
   const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-  Chunks<DT, AKC, PA> ca[2];
-  Chunks<DT, BKC, PB> cb[2];
-  KeptChunks ck[2];
+  Chunks<DT, AKC, PA> ca;
+  Chunks<DT, BKC, PB> cb;
+  KeptChunks ck;
   Reader<AKC, kAnyTile, 2, kAnyK> ra;
   Reader<BKC, kAnyTile, 2, kAnyK> rb;
   ra.init(wm, lane);
@@ -1058,16 +1112,20 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
   float bs[2] = {0.0f, 0.0f};
   const int64_t all = ((int64_t)K + kAnyK - 1) / kAnyK;
   const int64_t s0 = (int64_t)blockIdx.y * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
+  ca.init(A, m0, M, s0 * kAnyK, t);
+  if (B8) ck.init(BK, n0, s0 * kAnyK, t);
+  else cb.init(B, n0, N, s0 * kAnyK, t);
   auto fetch = [&](int64_t s, int set) {
-    ca[set].fetch(A, m0, M, s * kAnyK, K, t);
-    if (B8) ck[set].fetch(BK, n0, N, s * kAnyK, K, t);
-    else cb[set].fetch(B, n0, N, s * kAnyK, K, t);
+    const int64_t left = K - s * kAnyK;
+    ca.fetch(set, left, t);
+    if (B8) ck.fetch(set, left, t);
+    else cb.fetch(set, left, t);
   };
   auto step = [&](int64_t s, int set) {
     __syncthreads();
-    ca[set].put(lds, t);
-    if (B8) ck[set].put(lds + PA * kPlane, BK.fmt, t);
-    else cb[set].put(lds + PA * kPlane, t);
+    ca.put(set, lds, t);
+    if (B8) ck.put(set, lds + PA * kPlane, BK.fmt, t);
+    else cb.put(set, lds + PA * kPlane, t);
     __syncthreads();
     if (s + 2 < s1) fetch(s + 2, set);
 #pragma unroll

@@ -108,7 +108,8 @@ struct Cost {
 Cost cost_of_form(int form, bool wgrad, bool f32) {
   if (form == kLarge) return {256, kBK, 1, 1.1, wgrad ? 1.8 : 1.7, wgrad ? 17.0 : 10.0};
   if (form == kSmall) return {128, kBK, 2, wgrad ? 0.9 : 0.45, wgrad ? 1.3 : 0.95, 6.0};
-  return {kAnyTile, kAnyK, 2, f32 && !wgrad ? 2.3 : 1.5, f32 && !wgrad ? 3.3 : 2.1, 5.0};
+  if (f32) return {kAnyTile, kAnyK, 2, wgrad ? 1.4 : 2.2, wgrad ? 2.1 : 3.3, 5.0};
+  return {kAnyTile, kAnyK, 2, wgrad ? 0.8 : 0.6, 1.1, 5.0};
 }
 
 double cost_of(const Cost& c, int64_t M, int64_t N, int64_t splits, int64_t per) {

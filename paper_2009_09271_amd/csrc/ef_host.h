@@ -27,11 +27,12 @@ bool timing_slot(const char* name, hipEvent_t* a, hipEvent_t* b);
 
 }  // namespace efs
 
-// Every launch goes through this macro: the kernel is named after its expression.
-#define EF_LAUNCH(KERNEL, GRID, BLOCK, SHM, ST, ...)                                   \
+// Every launch goes through this macro: the kernel is named after its expression, or NAME (static storage).
+#define EF_LAUNCH(KERNEL, GRID, BLOCK, SHM, ST, ...) EF_LAUNCH_AS(#KERNEL, KERNEL, GRID, BLOCK, SHM, ST, __VA_ARGS__)
+#define EF_LAUNCH_AS(NAME, KERNEL, GRID, BLOCK, SHM, ST, ...)                          \
   do {                                                                                 \
     hipEvent_t _ea = nullptr, _eb = nullptr;                                           \
-    if (efs::timing_slot(#KERNEL, &_ea, &_eb))                                         \
+    if (efs::timing_slot(NAME, &_ea, &_eb))                                            \
       hipExtLaunchKernelGGL(KERNEL, GRID, BLOCK, SHM, ST, _ea, _eb, 0u, __VA_ARGS__); \
     else                                                                               \
       hipLaunchKernelGGL(KERNEL, GRID, BLOCK, SHM, ST, __VA_ARGS__);                  \

@@ -152,6 +152,13 @@ size_t product_bytes(bool wgrad, int dtype, int64_t M, int64_t N, int64_t K) {
   return splits == 1 ? 0 : align_up((size_t)splits * ((size_t)M * padded(N) + (size_t)M) * 4, kAlign);
 }
 
+// Names of the products' launches in the timing records, by kernel and kind.
+constexpr const char* kLabel[4][3] = {
+    {"k_linear_bf16<256> forward", "k_linear_bf16<256> dgrad", "k_linear_bf16<256> wgrad"},
+    {"k_linear_bf16<128> forward", "k_linear_bf16<128> dgrad", "k_linear_bf16<128> wgrad"},
+    {"k_linear_any forward", "k_linear_any dgrad", "k_linear_any wgrad"},
+    {"k_linear_join forward", "k_linear_join dgrad", "k_linear_join wgrad"}};
+
 template <int KIND, int DT, int DO>
 int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
   const size_t need = product_bytes(KIND == K_WGRAD, DT, p.M, p.N, p.K);
@@ -165,7 +172,7 @@ int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
       // (32 outputs a workgroup where a group of the checkpoint needs them, or where half the workgroups fill the CUs)
       const int ot = p.ep.k.codes || p.N >= 16 * 4 * kCUs ? 2 : 1;
       const dim3 grid((unsigned)((p.N + 16 * ot - 1) / (16 * ot))), blk(kFewWaves * 64);
-#define EF_FEW(TT, OT) EF_LAUNCH((k_linear_few<TT, OT>), grid, blk, 0, st, (int32_t)p.M, (int32_t)p.N, (int32_t)p.K, p.A, p.B, p.ep)
+#define EF_FEW(TT, OT) EF_LAUNCH_AS("k_linear_few forward", (k_linear_few<TT, OT>), grid, blk, 0, st, (int32_t)p.M, (int32_t)p.N, (int32_t)p.K, p.A, p.B, p.ep)
       if (p.M <= 16 && ot == 1) EF_FEW(1, 1);
       else if (p.M <= 16) EF_FEW(1, 2);
       else if (ot == 1) EF_FEW(2, 1);
@@ -187,13 +194,13 @@ int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
 #define EF_FORM(FMT)                                                                                                  \
   do {                                                                                                                \
     if (pl.form == kLarge)                                                                                            \
-      EF_LAUNCH((k_linear_bf16<KIND, DO, FMT, 256, 256, 2, 4>), grid, dim3(512), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp); \
+      EF_LAUNCH_AS(kLabel[0][KIND], (k_linear_bf16<KIND, DO, FMT, 256, 256, 2, 4>), grid, dim3(512), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp); \
     else                                                                                                              \
-      EF_LAUNCH((k_linear_bf16<KIND, DO, FMT, 128, 128, 2, 2>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp); \
+      EF_LAUNCH_AS(kLabel[1][KIND], (k_linear_bf16<KIND, DO, FMT, 128, 128, 2, 2>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp); \
   } while (0)
   if constexpr (DT == EF_BF16) {
     if (pl.form == kAny) {
-      EF_LAUNCH((k_linear_any<KIND, DT, DO>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
+      EF_LAUNCH_AS(kLabel[2][KIND], (k_linear_any<KIND, DT, DO>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
     } else if constexpr (KIND == K_WGRAD) {
       if (p.BK.fmt == EF_CKPT_E4M3) EF_FORM(EF_CKPT_E4M3);
       else EF_FORM(EF_CKPT_INT8);
@@ -201,13 +208,13 @@ int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
       EF_FORM(EF_CKPT_INT8);  // (read no checkpoint along k)
     }
   } else {
-    EF_LAUNCH((k_linear_any<KIND, DT, DO>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
+    EF_LAUNCH_AS(kLabel[2][KIND], (k_linear_any<KIND, DT, DO>), grid, dim3(256), 0, st, M, N, K, p.A, p.B, p.BK, p.ep, sp);
   }
 #undef EF_FORM
   EF_TRY(launched());
   if (pl.splits == 1) return EF_OK;
   const int64_t lanes = p.M * (sp.Np / 8) + (KIND == K_WGRAD && p.ep.db ? p.M : 0);
-  EF_LAUNCH((k_linear_join<KIND, DO>), dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, st, M, N, (int)pl.splits, sp, p.ep);
+  EF_LAUNCH_AS(kLabel[3][KIND], (k_linear_join<KIND, DO>), dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, st, M, N, (int)pl.splits, sp, p.ep);
   return launched();
 }
 

@@ -595,3 +595,142 @@ def test_refuses_a_short_workspace():
         assert ex.value.code == code
     torch.cuda.synchronize()
     assert bool((dw == 3.0).all())
+
+
+# ---- large products ------------------------------------------------------------------------------------------------------
+def gpu_ints(seed, *shape):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randint(-3, 4, shape, generator=g, device="cuda", dtype=torch.int8)
+
+
+def strided(x, dtype, ld):
+    """x as `dtype` with rows ld apart."""
+    import torch
+    t = torch.zeros(x.shape[0] * ld, dtype=tt(dtype), device="cuda").view(x.shape[0], ld)[:, :x.shape[1]]
+    t.copy_(x)
+    return t
+
+
+def pack_ints(x, fmt):
+    """The checkpoint of small whole numbers, which both formats hold exactly."""
+    q, s = E().ckpt_buffers(*x.shape)
+    E().ef_ckpt_pack(x.float().contiguous(), q, s, fmt)
+    return q, s
+
+
+def mm64(a, b):
+    import torch
+    return torch.matmul(a.double().contiguous(), b.double().contiguous())
+
+
+@pytest.mark.parametrize("dtype,n,a,b", [("bf16", 4090, 1032, 4088), ("bf16", 2301, 2056, 2048), ("bf16", 3000, 1001, 999),
+                                         ("f32", 1500, 600, 1100), ("bf16", 640, 4096, 8)])
+def test_large_products_of_integers(dtype, n, a, b):
+    """All three products at sizes of many tiles, each with a ragged edge: bit for bit."""
+    import torch
+    announce("large ints", dtype, n, a, b)
+    e = E()
+    t = tt(dtype)
+    x, w, r = gpu_ints(1, n, a), gpu_ints(2, b, a), gpu_ints(3, n, b)
+    y = torch.empty(n, b, dtype=t, device="cuda")
+    e.ef_linear_forward(x.to(t), w.to(t), y, ws(e.EF_OP_FORWARD, n, a, b, dtype), act=L.RELU, res=r.to(t))
+    assert torch.equal(y, (mm64(x, w.t()).clamp(min=0) + r).to(t))
+    # back: dy [n][a], weight [a][b], the kept input of an activation [n][b]
+    dy, wt, z = x, gpu_ints(4, a, b), gpu_ints(5, n, b)
+    for fmt in FMTS:
+        q, s = pack_ints(z, fmt)
+        dx = torch.empty(n, b, dtype=t, device="cuda")
+        e.ef_linear_dgrad(dy.to(t), wt.to(t), dx, ws(e.EF_OP_DGRAD, n, b, a, dtype), act=L.RELU, codes=q, scales=s, fmt=fmt, res=r.to(t))
+        assert torch.equal(dx, (mm64(dy, wt) * (z > 0) + r).to(t))
+    # weights [b][n], their gradient summed over a tokens
+    dy, k = gpu_ints(6, a, b), gpu_ints(7, a, n)
+    want, wb = mm64(dy.t(), k).float(), dy.double().sum(0).float()
+    for fmt in FMTS:
+        q, s = pack_ints(k, fmt)
+        wk = ws(e.EF_OP_WGRAD, a, n, b, dtype)
+        dw, db = torch.full((b, n), 2.0, device="cuda"), torch.full((b,), 2.0, device="cuda")
+        e.ef_linear_wgrad(dy.to(t), q, s, fmt, dw, wk, db=db, accumulate=True)
+        assert torch.equal(dw, want + 2.0) and torch.equal(db, wb + 2.0)
+        h, hb = torch.empty(b, n, dtype=torch.bfloat16, device="cuda"), torch.empty(b, dtype=torch.bfloat16, device="cuda")
+        e.ef_linear_wgrad(dy.to(t), q, s, fmt, h, wk, db=hb)
+        assert torch.equal(h, want.bfloat16()) and torch.equal(hb, wb.bfloat16())
+
+
+@pytest.mark.parametrize("ld", [1 << 21, (1 << 21) + 8])
+def test_rows_far_apart(ld):
+    """Leading dimensions at and past the one up to which a tile's offsets are taken in 32 bits."""
+    import torch
+    e = E()
+    n, i, o = 300, 64, 72
+    announce("rows", ld, "apart")
+    x, w, dy = gpu_ints(1, n, i), gpu_ints(2, o, i), gpu_ints(3, n, o)
+    y, dx = torch.empty(n, o, dtype=torch.bfloat16, device="cuda"), torch.empty(n, i, dtype=torch.bfloat16, device="cuda")
+    wide = strided(x, "bf16", ld)
+    e.ef_linear_forward(wide, w.bfloat16(), y, ws(e.EF_OP_FORWARD, n, i, o, "bf16"))
+    assert torch.equal(y, mm64(x, w.t()).bfloat16())
+    q, s = e.ckpt_buffers(n, i)
+    e.ef_ckpt_pack(wide, q, s)
+    del wide
+    wide = strided(w, "bf16", ld)
+    e.ef_linear_dgrad(dy.bfloat16(), wide, dx, ws(e.EF_OP_DGRAD, n, i, o, "bf16"))
+    assert torch.equal(dx, mm64(dy, w).bfloat16())
+    del wide
+    wide = strided(dy, "bf16", ld)
+    dw = torch.empty(o, i, device="cuda")
+    e.ef_linear_wgrad(wide, q, s, L.INT8, dw, ws(e.EF_OP_WGRAD, n, i, o, "bf16"))
+    assert torch.equal(dw, mm64(dy.t(), x).float())
+
+
+def test_products_past_32_bit_offsets():
+    import torch
+    e = E()
+    n, k, m = 40000, 64, 65536
+    announce("products of", n, "x", m)
+    x, w = gpu_ints(1, n, k), gpu_ints(2, m, k)
+    rows = torch.tensor([0, 255, 256, 32767, 32768, n - 1], device="cuda")
+    y = torch.empty(n, m, dtype=torch.bfloat16, device="cuda")
+    q, s = e.ckpt_buffers(n, m)
+    e.ef_linear_forward(x.bfloat16(), w.bfloat16(), y, ws(e.EF_OP_FORWARD, n, k, m, "bf16"), codes=q, scales=s)
+    want = mm64(x[rows], w.t())
+    assert torch.equal(y[rows], want.bfloat16())
+    z = torch.empty(len(rows), m, device="cuda")
+    e.ef_ckpt_unpack(q[rows].contiguous(), s[rows].contiguous(), L.INT8, z)
+    step = torch.exp2((s[rows].double() - 127).floor()).repeat_interleave(32, 1)
+    assert bool(((z.double() - want).abs() <= step / 2).all())
+    # back through the activation that these were kept of: dy [n][k], weight [k][m]
+    wt = gpu_ints(3, k, m)
+    e.ef_linear_dgrad(x.bfloat16(), wt.bfloat16(), y, ws(e.EF_OP_DGRAD, n, m, k, "bf16"), act=L.RELU, codes=q, scales=s)
+    assert torch.equal(y[rows], (mm64(x[rows], wt) * (z > 0)).bfloat16())
+    del y, q, s
+    dy, c = gpu_ints(4, k, n), gpu_ints(5, k, m)
+    q, s = pack_ints(c, L.E4M3)
+    dw = torch.zeros(n, m, device="cuda")
+    e.ef_linear_wgrad(dy.bfloat16(), q, s, L.E4M3, dw, ws(e.EF_OP_WGRAD, k, m, n, "bf16"), accumulate=True)
+    assert torch.equal(dw[rows], mm64(dy[:, rows].t(), c).float())
+
+
+def test_two_streams_at_once_and_twice_the_same():
+    """Products that run at the same time in workspaces of their own, and again: bitwise the same."""
+    import torch
+    e = E()
+    n, i, o = 2000, 512, 384
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    dy = torch.randn(n, o, generator=g, device="cuda").bfloat16()
+    q, s = e.ckpt_buffers(n, i)
+    e.ef_ckpt_pack(torch.randn(n, i, generator=g, device="cuda"), q, s)
+    wsp = [ws(e.EF_OP_WGRAD, n, i, o, "bf16") for _ in range(2)]
+    dw = [torch.empty(o, i, device="cuda") for _ in range(3)]
+    e.ef_linear_wgrad(dy, q, s, 0, dw[2], wsp[0])
+    torch.cuda.synchronize()
+    side = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for k in range(2):
+            dw[k].fill_(float("nan"))
+        torch.cuda.synchronize()
+        for k in range(2):
+            e.ef_linear_wgrad(dy, q, s, 0, dw[k], wsp[k], stream=side[k])
+        torch.cuda.synchronize()
+        assert torch.equal(dw[0], dw[2]) and torch.equal(dw[1], dw[2])

@@ -512,8 +512,8 @@ def _refuse(t, name, where, dtypes, dev, n, c):
         why = f"{name} is None" if t is None else f"{name} is not a tensor"
     elif not t.is_cuda:
         why = f"{name} is not on a GPU"
-    elif dev is not None and t.device != dev:
-        why = f"{name} is on {t.device}, not on {dev}"
+    elif dev is not None and t.get_device() != dev:
+        why = f"{name} is on {t.device}, not on cuda:{dev}"
     elif t.dtype not in dtypes:
         why = f"{name} has dtype {t.dtype}"
     elif n == -1:
@@ -529,10 +529,10 @@ def _refuse(t, name, where, dtypes, dev, n, c):
 
 def _mat(t, name, where, dtypes, dev=None, n=None, c=None):
     """Checks a matrix argument before its pointer crosses the ABI; its elements from one row to the next (a single
-    row's own length, whatever its stride says)."""
+    row's own length, whatever its stride says).  dev: the number of the GPU that it has to be on."""
     try:
         (rows, cols), (ld, one) = t.shape, t.stride()
-        fits = (t.dtype in dtypes and t.is_cuda and (dev is None or t.device == dev) and (n is None or rows == n)
+        fits = (t.dtype in dtypes and (t.is_cuda if dev is None else t.get_device() == dev) and (n is None or rows == n)
                 and (c is None or cols == c) and (one == 1 or cols <= 1) and (ld >= cols or rows <= 1))
     except (AttributeError, TypeError, ValueError):
         fits = False
@@ -542,15 +542,14 @@ def _mat(t, name, where, dtypes, dev=None, n=None, c=None):
 
 
 def _vec(t, name, where, dtypes, dev, c):
-    if not (getattr(t, "dtype", None) in dtypes and t.device == dev and t.shape == (c,) and (c <= 1 or t.stride(0) == 1)):
+    if not (getattr(t, "dtype", None) in dtypes and t.get_device() == dev and t.shape == (c,) and (c <= 1 or t.stride(0) == 1)):
         _refuse(t, name, where, dtypes, dev, -1, c)
 
 
 def _kept(codes, scales, n, c, where, dev):
     g = (c + 31) // 32
-    for t, name, w in ((codes, "codes", 32 * g), (scales, "scales", g)):
-        if _mat(t, name, where, _U8, dev, n, w) != w:
-            raise EfError(EF_EINVAL, where, f"{name} is not contiguous")
+    if _mat(codes, "codes", where, _U8, dev, n, 32 * g) != 32 * g or _mat(scales, "scales", where, _U8, dev, n, g) != g:
+        raise EfError(EF_EINVAL, where, "codes or scales are not contiguous")
     return codes.data_ptr(), scales.data_ptr()
 
 
@@ -561,14 +560,14 @@ if _torch is not None:
 
 
 def _enqueue(fn, where, dev, stream, *args):
-    """Calls the library with device `dev` current, on `stream` or that device's current stream."""
-    if dev.index != _torch.cuda.current_device():
+    """Calls the library with GPU `dev` current, on `stream` or that GPU's current stream."""
+    if dev != _torch.cuda.current_device():
         with _torch.cuda.device(dev):
             return _enqueue(fn, where, dev, stream, *args)
     if stream is not None:
         st = stream.cuda_stream
     elif _raw_stream is not None:
-        st = _raw_stream(dev.index)
+        st = _raw_stream(dev)
     else:
         st = _torch.cuda.current_stream(dev).cuda_stream
     code = fn(*args, st)
@@ -597,16 +596,16 @@ def linear_workspace(op, n, i, o, dtype, device="cuda"):
 def _ws(ws, where, dev):
     if ws is None:
         return 0, 0
-    if not ws.is_cuda or ws.device != dev or not ws.is_contiguous():
-        raise EfError(EF_EINVAL, where, f"ws is not a contiguous tensor on {dev}")
-    return ws.data_ptr(), _nbytes(ws)
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise EfError(EF_EINVAL, where, f"ws is not a contiguous tensor on cuda:{dev}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def ef_ckpt_pack(x, codes, scales, fmt=EF_CKPT_INT8, stream=None):
     """codes, scales = the 8-bit checkpoint of x [n][c]."""
     w = "ef_ckpt_pack"
     ld = _mat(x, "x", w, _MATS)
-    (n, c), dev = x.shape, x.device
+    (n, c), dev = x.shape, x.get_device()
     q, s = _kept(codes, scales, n, c, w, dev)
     _enqueue(_lib.ef_ckpt_pack, w, dev, stream, n, c, x.data_ptr(), ld, _CODE[x.dtype], fmt, q, s)
 
@@ -615,7 +614,7 @@ def ef_ckpt_unpack(codes, scales, fmt, y, stream=None):
     """y [n][c] = what a checkpoint stands for."""
     w = "ef_ckpt_unpack"
     ld = _mat(y, "y", w, _MATS)
-    (n, c), dev = y.shape, y.device
+    (n, c), dev = y.shape, y.get_device()
     q, s = _kept(codes, scales, n, c, w, dev)
     _enqueue(_lib.ef_ckpt_unpack, w, dev, stream, n, c, q, s, fmt, y.data_ptr(), ld, _CODE[y.dtype])
 
@@ -624,7 +623,7 @@ def ef_ckpt_act_backward(act, codes, scales, fmt, dy, dz, stream=None):
     """dz = dy * act'(z), z the kept input of the activation; dz may be dy."""
     w = "ef_ckpt_act_backward"
     ld = _mat(dy, "dy", w, _MATS)
-    (n, c), dev, t = dy.shape, dy.device, dy.dtype
+    (n, c), dev, t = dy.shape, dy.get_device(), dy.dtype
     ldz = _mat(dz, "dz", w, (t,), dev, n, c)
     q, s = _kept(codes, scales, n, c, w, dev)
     _enqueue(_lib.ef_ckpt_act_backward, w, dev, stream, n, c, act, q, s, fmt, dy.data_ptr(), ld, dz.data_ptr(), ldz, _CODE[t])
@@ -636,7 +635,7 @@ def ef_linear_forward(x, weight, y, ws, bias=None, act=EF_ACT_NONE, res=None, co
     x [n][i], weight [o][i], y and res [n][o], bias [o]; res may be y."""
     w = "ef_linear_forward"
     ldx = _mat(x, "x", w, _MATS)
-    (n, i), dev, dtypes = x.shape, x.device, (x.dtype,)
+    (n, i), dev, dtypes = x.shape, x.get_device(), (x.dtype,)
     ldw = _mat(weight, "weight", w, dtypes, dev, None, i)
     o = weight.shape[0]
     ldy = _mat(y, "y", w, dtypes, dev, n, o)
@@ -658,7 +657,7 @@ def ef_linear_dgrad(dy, weight, dx, ws, act=EF_ACT_NONE, codes=None, scales=None
     dy [n][o], weight [o][i], dx and res [n][i]; res may be dx."""
     w = "ef_linear_dgrad"
     ldy = _mat(dy, "dy", w, _MATS)
-    (n, o), dev, dtypes = dy.shape, dy.device, (dy.dtype,)
+    (n, o), dev, dtypes = dy.shape, dy.get_device(), (dy.dtype,)
     ldw = _mat(weight, "weight", w, dtypes, dev, o)
     i = weight.shape[1]
     ldx = _mat(dx, "dx", w, dtypes, dev, n, i)
@@ -676,7 +675,7 @@ def ef_linear_wgrad(dy, codes, scales, fmt, dw, ws, db=None, accumulate=False, s
     dy [n][o], dw [o][i] contiguous (a segment of the flat gradient or of the error-feedback memory), db [o]."""
     w = "ef_linear_wgrad"
     ldy = _mat(dy, "dy", w, _MATS)
-    (n, o), dev = dy.shape, dy.device
+    (n, o), dev = dy.shape, dy.get_device()
     ldw = _mat(dw, "dw", w, _MATS, dev, o)
     i = dw.shape[1]
     if ldw != i:

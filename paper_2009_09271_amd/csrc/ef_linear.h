@@ -462,6 +462,7 @@ struct Split {
   int64_t plane;   // M * Np
   int32_t Np;
   int32_t per;     // steps per split
+  int32_t splits;
 };
 
 // A wavefront's T times 32 x 64 of C, handed over R times 32 rows at a time through its own part of the LDS (a
@@ -472,7 +473,7 @@ constexpr int kSlabPitch = 68;
 constexpr int slab_bytes(int waves, int R) { return waves * R * 32 * kSlabPitch * 4; }
 template <int KIND, int DO, int T, int R>
 __device__ __forceinline__ void finish(const f32x16 (&acc)[T][2], char* lds, int wave, int lane, int64_t row0, int64_t col0, int32_t M,
-                                       int32_t N, const Epi& ep, const Split& sp) {
+                                       int32_t N, const Epi& ep, const Split& sp, int64_t split) {
   float* slab = reinterpret_cast<float*>(lds) + wave * R * 32 * kSlabPitch;
   const int32_t col = (int32_t)col0 + (lane & 7) * 8;
   const float* from = slab + (lane >> 3) * kSlabPitch + (lane & 7) * 8;
@@ -492,7 +493,7 @@ __device__ __forceinline__ void finish(const f32x16 (&acc)[T][2], char* lds, int
       const f32x4 hi = *reinterpret_cast<const f32x4*>(from + q * 8 * kSlabPitch + 4);
       if (sp.part) {
         if (row < M && col < sp.Np) {
-          float* to = sp.part + blockIdx.y * sp.plane + row * sp.Np + col;
+          float* to = sp.part + split * sp.plane + row * sp.Np + col;
           *reinterpret_cast<f32x4*>(to) = lo;
           *reinterpret_cast<f32x4*>(to + 4) = hi;
         }
@@ -523,13 +524,14 @@ __device__ __forceinline__ void finish(const f32x16 (&acc)[T][2], char* lds, int
 
 // wgrad, the wavefronts of the first column of tiles: the sums of A's lines that went by; two lanes hold a line.
 template <int DO, int T>
-__device__ __forceinline__ void finish_db(const float (&s)[T], int lane, int64_t m0, int32_t M, const Epi& ep, const Split& sp) {
+__device__ __forceinline__ void finish_db(const float (&s)[T], int lane, int64_t m0, int32_t M, const Epi& ep, const Split& sp,
+                                          int64_t split) {
 #pragma unroll
   for (int a = 0; a < T; ++a) {
     const float t = s[a] + __shfl_xor(s[a], 32);
     const int64_t m = m0 + a * 32 + lane;
     if (lane < 32 && m < M) {
-      if (sp.part) sp.part_db[(int64_t)blockIdx.y * M + m] = t;
+      if (sp.part) sp.part_db[split * M + m] = t;
       else store_db<DO>(ep, m, t);
     }
   }
@@ -743,14 +745,17 @@ __device__ __forceinline__ float add8(bf16x8 f, float s) {
   return s;
 }
 
-// Tiles in an order in which those that run at one time on an XCD (workgroups b, b + 8, b + 16, ...) are
-// neighbours: each XCD has a run of the tiles, in bands of eight rows of tiles.
-__device__ __forceinline__ void tile_of(uint32_t b, uint32_t tm, uint32_t tn, uint32_t* m, uint32_t* n) {
-  const uint32_t T = tm * tn, q = T / 8, rest = T % 8, x = b % 8;
-  const uint32_t id = x * q + (x < rest ? x : rest) + b / 8;
-  const uint32_t band = id / (8 * tn), h = tm - band * 8 < 8 ? tm - band * 8 : 8, in = id - band * 8 * tn;
-  *m = band * 8 + in % h;
-  *n = in / h;
+// What workgroup b of a product does: a tile of C and a part of k.  In an order in which those that run at one time on an
+// XCD (workgroups b, b + 8, b + 16, ...) share what they read: each XCD has a run of the work, one part of k after the
+// other, its tiles in bands of eight rows of tiles.
+struct Share {
+  uint32_t m, n, z;
+};
+__device__ __forceinline__ Share share_of(uint32_t b, uint32_t tm, uint32_t tn, uint32_t splits) {
+  const uint32_t tiles = tm * tn, T = tiles * splits, q = T / 8, rest = T % 8, x = b % 8;
+  const uint32_t id = x * q + (x < rest ? x : rest) + b / 8, z = id / tiles, t = id - z * tiles;
+  const uint32_t band = t / (8 * tn), h = tm - band * 8 < 8 ? tm - band * 8 : 8, in = t - band * 8 * tn;
+  return {band * 8 + in % h, in / h, z};
 }
 
 template <int KIND, int DO, int FMT, int BM, int BN, int WM, int WN>
@@ -761,11 +766,10 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
   constexpr int kA = BM * kBK * 2, kB = BN * kBK * 2;
   __shared__ __align__(1024) char lds[3 * kA + 2 * kB];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  uint32_t ti, tj;
-  tile_of(blockIdx.x, ((uint32_t)M + BM - 1) / BM, ((uint32_t)N + BN - 1) / BN, &ti, &tj);
-  const int64_t m0 = (int64_t)ti * BM, n0 = (int64_t)tj * BN;
+  const Share my = share_of(blockIdx.x, ((uint32_t)M + BM - 1) / BM, ((uint32_t)N + BN - 1) / BN, sp.splits);
+  const int64_t m0 = (int64_t)my.m * BM, n0 = (int64_t)my.n * BN;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * 64;
-  const int all = (K + kBK - 1) / kBK, s0 = (int)blockIdx.y * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
+  const int all = (K + kBK - 1) / kBK, s0 = (int)my.z * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
 
   Stream<AKC, BM, NW> sa;
   sa.init(A, m0, M, K, wave, lane);
@@ -936,11 +940,11 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
       for (int a = 0; a < TM; ++a)
 #pragma unroll
         for (int z = 1; z < WN; ++z) bs[a] += share[((wave + z) * TM + a) * 64 + lane];
-      finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
+      finish_db<DO>(bs, lane, m0 + wm, M, ep, sp, my.z);
     }
     __syncthreads();
   }
-  finish<KIND, DO, TM, 2>(acc, lds, wave, lane, m0 + wm, n0 + wn, M, N, ep, sp);
+  finish<KIND, DO, TM, 2>(acc, lds, wave, lane, m0 + wm, n0 + wn, M, N, ep, sp, my.z);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1090,9 +1094,8 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
   constexpr int kTiles = (PA + PB) * kPlane, kSlabs = slab_bytes(4, 1);
   __shared__ __align__(1024) char lds[kTiles > kSlabs ? kTiles : kSlabs];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  uint32_t ti, tj;
-  tile_of(blockIdx.x, ((uint32_t)M + kAnyTile - 1) / kAnyTile, ((uint32_t)N + kAnyTile - 1) / kAnyTile, &ti, &tj);
-  const int64_t m0 = (int64_t)ti * kAnyTile, n0 = (int64_t)tj * kAnyTile;
+  const Share my = share_of(blockIdx.x, ((uint32_t)M + kAnyTile - 1) / kAnyTile, ((uint32_t)N + kAnyTile - 1) / kAnyTile, sp.splits);
+  const int64_t m0 = (int64_t)my.m * kAnyTile, n0 = (int64_t)my.n * kAnyTile;
   const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
   Chunks<DT, AKC, PA> ca;
   Chunks<DT, BKC, PB> cb;
@@ -1111,7 +1114,7 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
   const bool sums = KIND == K_WGRAD && ep.db && n0 == 0 && wn == 0;
   float bs[2] = {0.0f, 0.0f};
   const int64_t all = ((int64_t)K + kAnyK - 1) / kAnyK;
-  const int64_t s0 = (int64_t)blockIdx.y * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
+  const int64_t s0 = (int64_t)my.z * sp.per, s1 = s0 + sp.per < all ? s0 + sp.per : all;
   ca.init(A, m0, M, s0 * kAnyK, t);
   if (B8) ck.init(BK, n0, s0 * kAnyK, t);
   else cb.init(B, n0, N, s0 * kAnyK, t);
@@ -1164,8 +1167,8 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
     if (s + 1 < s1) step(s + 1, 1);
   }
   __syncthreads();
-  finish<KIND, DO, 2, 1>(acc, lds, wave, lane, m0 + wm, n0 + wn, M, N, ep, sp);
-  if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp);
+  finish<KIND, DO, 2, 1>(acc, lds, wave, lane, m0 + wm, n0 + wn, M, N, ep, sp, my.z);
+  if (sums) finish_db<DO>(bs, lane, m0 + wm, M, ep, sp, my.z);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1245,7 +1248,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_linear_few(int32_t n, int32_
 
 // The splits' sums in order, then the epilogue.  Np / 8 lanes a row, whole groups side by side.
 template <int KIND, int DO>
-__global__ __launch_bounds__(256) void k_linear_join(int32_t M, int32_t N, int splits, Split sp, Epi ep) {
+__global__ __launch_bounds__(256) void k_linear_join(int32_t M, int32_t N, Split sp, Epi ep) {
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int32_t w = sp.Np / 8;
   const int64_t row = id / w;
@@ -1255,7 +1258,7 @@ __global__ __launch_bounds__(256) void k_linear_join(int32_t M, int32_t N, int s
     const int64_t m = id - (int64_t)M * w;
     if (!ep.db || m >= M) return;
     float t = 0.0f;
-    for (int z = 0; z < splits; ++z) t += sp.part_db[(int64_t)z * M + m];
+    for (int z = 0; z < sp.splits; ++z) t += sp.part_db[(int64_t)z * M + m];
     store_db<DO>(ep, m, t);
     return;
   }
@@ -1265,7 +1268,7 @@ __global__ __launch_bounds__(256) void k_linear_join(int32_t M, int32_t N, int s
   load_bias<KIND, DO>(ep, col, N, b);
   side.load(ep, row, col, cnt);
   if (in)
-    for (int z = 0; z < splits; ++z) {
+    for (int z = 0; z < sp.splits; ++z) {
       const float* p = sp.part + z * sp.plane + row * sp.Np + col;
       const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
 #pragma unroll

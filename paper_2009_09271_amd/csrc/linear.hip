@@ -183,13 +183,13 @@ int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
   }
   const Plan pl = plan_of(fast, KIND == K_WGRAD, DT == EF_F32, p.M, p.N, p.K);
   const int64_t tile = pl.form == kLarge ? 256 : 128, tiles = ((p.M + tile - 1) / tile) * ((p.N + tile - 1) / tile);
-  if (tiles > kMaxGrid) return EF_ERANGE;
-  Split sp{nullptr, nullptr, p.M * padded(p.N), padded(p.N), pl.per};
+  if (tiles * pl.splits > kMaxGrid) return EF_ERANGE;
+  Split sp{nullptr, nullptr, p.M * padded(p.N), padded(p.N), pl.per, pl.splits};
   if (pl.splits > 1) {
     sp.part = static_cast<float*>(ws);
     sp.part_db = sp.part + (int64_t)pl.splits * sp.plane;
   }
-  const dim3 grid((unsigned)tiles, (unsigned)pl.splits);
+  const dim3 grid((unsigned)(tiles * pl.splits));
   const int32_t M = (int32_t)p.M, N = (int32_t)p.N, K = (int32_t)p.K;
 #define EF_FORM(FMT)                                                                                                  \
   do {                                                                                                                \
@@ -214,7 +214,7 @@ int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
   EF_TRY(launched());
   if (pl.splits == 1) return EF_OK;
   const int64_t lanes = p.M * (sp.Np / 8) + (KIND == K_WGRAD && p.ep.db ? p.M : 0);
-  EF_LAUNCH_AS(kLabel[3][KIND], (k_linear_join<KIND, DO>), dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, st, M, N, (int)pl.splits, sp, p.ep);
+  EF_LAUNCH_AS(kLabel[3][KIND], (k_linear_join<KIND, DO>), dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, st, M, N, sp, p.ep);
   return launched();
 }
 

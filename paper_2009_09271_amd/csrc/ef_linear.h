@@ -959,6 +959,22 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
 constexpr int kAnyTile = 128, kAnyK = 32;
 constexpr int kPlane = kAnyTile * kAnyK * 2;
 
+// Eight float32 values as hi + mid + lo, each rounded to the nearest bfloat16.  hi is held at the largest one: a finite
+// value does not round to an infinity, and what is not finite goes on into mid and lo.
+__device__ __forceinline__ void split8(const Raw<EF_F32>& r, u32x4 (&w)[3]) {
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    float x = r.value(2 * h), y = r.value(2 * h + 1);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      w[p][h] = p ? f_bf16x2(x, y) : f_bf16x2(__builtin_amdgcn_fmed3f(x, -0x1.FEp127f, 0x1.FEp127f), __builtin_amdgcn_fmed3f(y, -0x1.FEp127f, 0x1.FEp127f));
+      x -= __uint_as_float(w[p][h] << 16);
+      y -= __uint_as_float(w[p][h] & 0xFFFF0000u);
+    }
+  }
+}
+__device__ __forceinline__ void split8(const Raw<EF_BF16>& r, u32x4 (&w)[3]) { w[0] = u32x4{r.r[0], r.r[1], r.r[2], r.r[3]}; }
+
 // Where a thread's two chunks of eight elements of a step lie: eight k of a line where KC, else eight lines of a k.
 template <bool KC>
 struct Places {
@@ -1023,18 +1039,7 @@ struct Chunks {
         *reinterpret_cast<u32x4*>(to) = u32x4{r.r[0], r.r[1], r.r[2], r.r[3]};
       } else {
         u32x4 w[3];
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          float x = r.value(2 * h), y = r.value(2 * h + 1);
-#pragma unroll
-          for (int p = 0; p < 3; ++p) {
-            // (hi is held at the largest bfloat16: a finite value does not round to an infinity, and what is not
-            // finite goes on into mid and lo)
-            w[p][h] = p ? f_bf16x2(x, y) : f_bf16x2(__builtin_amdgcn_fmed3f(x, -0x1.FEp127f, 0x1.FEp127f), __builtin_amdgcn_fmed3f(y, -0x1.FEp127f, 0x1.FEp127f));
-            x -= __uint_as_float(w[p][h] << 16);
-            y -= __uint_as_float(w[p][h] & 0xFFFF0000u);
-          }
-        }
+        split8(r, w);
 #pragma unroll
         for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(to + p * kPlane) = w[p];
       }
@@ -1175,21 +1180,22 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
 // The forward product of a few tokens (up to 16 TT): the weights are read once, and that bounds it.  A workgroup
 // has 16 OT output features and splits k over its eight wavefronts; each takes the weights' rows as the first
 // operand and the tokens as the second, straight from memory to registers, 16 bytes a lane, eight loads of the
-// weights in flight.  The eight partial sums are added in order through the LDS.
+// weights in flight (sixteen, or past the caches: no faster); float32 as in k_linear_any.  4096 x 4096 weights in bfloat16,
+// one token: 8.1 us, 4.2 TB/s, of which 3 us are the launch and the last loads' latency.  The eight partial sums are added in order through the LDS.
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewWaves = 8;
 constexpr int kFewTokens = 32;
 
-template <int TT, int OT>
+template <int DT, int TT, int OT>
 __global__ __launch_bounds__(kFewWaves * 64) void k_linear_few(int32_t n, int32_t N, int32_t K, Mat X, Mat W, Epi ep) {
   __shared__ f32x4 red[kFewWaves][TT][OT][64];
-  constexpr int U = 8 / OT;
+  constexpr int S = DT == EF_F32 ? 4 : 2, P = DT == EF_F32 ? 3 : 1, U = 16 / S / OT;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t o0 = (int64_t)blockIdx.x * 16 * OT;
-  const int64_t ldw = W.ld * 2, ldx = X.ld * 2;
+  const int64_t ldw = W.ld * S, ldx = X.ld * S;
   const int64_t have = N - o0 < 16 * OT ? N - o0 : 16 * OT;
-  const auto rw = EF_BUFFER(static_cast<const char*>(W.p) + o0 * ldw, (have - 1) * ldw + (int64_t)K * 2);
-  const auto rx = EF_BUFFER(X.p, (int64_t)(n - 1) * ldx + (int64_t)K * 2);
+  const auto rw = EF_BUFFER(static_cast<const char*>(W.p) + o0 * ldw, (have - 1) * ldw + (int64_t)K * S);
+  const auto rx = EF_BUFFER(X.p, (int64_t)(n - 1) * ldx + (int64_t)K * S);
   const int kl = (lane >> 4) * 8;
   const int per = ((K + 32 * kFewWaves - 1) / (32 * kFewWaves) + 3) / 4 * 4;  // steps of 32 per wavefront: whole 256-byte runs
   const int c0 = wave * per, c1 = c0 + per;
@@ -1198,25 +1204,45 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_linear_few(int32_t n, int32_
   for (int t = 0; t < TT; ++t)
 #pragma unroll
     for (int o = 0; o < OT; ++o) acc[t][o] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  auto fetch = [&](auto r, int off, bool in) {
+    Raw<DT> v;
+#pragma unroll
+    for (int h = 0; h < S / 2; ++h) {
+      const u32x4 a = EF_BUFFER_B128(r, in ? off + h * 16 : kFar);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v.r[4 * h + j] = a[j];
+    }
+    return v;
+  };
   for (int c = c0; c < c1 && c * 32 < K; c += U) {
-    u32x4 w[U][OT], x[U][TT];
+    Raw<DT> w[U][OT], x[U][TT];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = (c + u) * 32 + kl;
       const bool in = k < K && c + u < c1;
 #pragma unroll
-      for (int o = 0; o < OT; ++o) w[u][o] = EF_BUFFER_B128(rw, in ? (int)((o * 16 + (lane & 15)) * ldw) + k * 2 : kFar);
+      for (int o = 0; o < OT; ++o) w[u][o] = fetch(rw, (int)((o * 16 + (lane & 15)) * ldw) + k * S, in);
 #pragma unroll
-      for (int t = 0; t < TT; ++t) x[u][t] = EF_BUFFER_B128(rx, in ? (int)((t * 16 + (lane & 15)) * ldx) + k * 2 : kFar);
+      for (int t = 0; t < TT; ++t) x[u][t] = fetch(rx, (int)((t * 16 + (lane & 15)) * ldx) + k * S, in);
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      u32x4 wp[OT][3], xp[TT][3];
 #pragma unroll
-      for (int o = 0; o < OT; ++o)
+      for (int o = 0; o < OT; ++o) split8(w[u][o], wp[o]);
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
-          acc[t][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[u][o]), __builtin_bit_cast(bf16x8, x[u][t]),
-                                                             acc[t][o], 0, 0, 0);
+      for (int t = 0; t < TT; ++t) split8(x[u][t], xp[t]);
+#pragma unroll
+      for (int d = P == 1 ? 0 : 2; d >= 0; --d)  // the least products first
+#pragma unroll
+        for (int p = 0; p <= d; ++p)
+#pragma unroll
+          for (int o = 0; o < OT; ++o)
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+              acc[t][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wp[o][p]), __builtin_bit_cast(bf16x8, xp[t][d - p]),
+                                                                 acc[t][o], 0, 0, 0);
+    }
   }
 #pragma unroll
   for (int t = 0; t < TT; ++t)
@@ -1240,10 +1266,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_linear_few(int32_t n, int32_
     }
   }
   float b[8];
-  Side<K_FWD, EF_BF16> side;
-  load_bias<K_FWD, EF_BF16>(ep, col, N, b);
+  Side<K_FWD, DT> side;
+  load_bias<K_FWD, DT>(ep, col, N, b);
   side.load(ep, token, col, cnt);
-  epilogue8<K_FWD, EF_BF16>(ep, token, col, cnt, v, b, side);
+  epilogue8<K_FWD, DT>(ep, token, col, cnt, v, b, side);
 }
 
 // The splits' sums in order, then the epilogue.  Np / 8 lanes a row, whole groups side by side.

@@ -86,6 +86,14 @@ bool fast_ok(const Product& p) {
   return KIND == K_WGRAD ? p.N <= kFastLd : fast_mat(p.B, KIND == K_FWD ? p.K : p.N);
 }
 
+// Few tokens: rows on 16 bytes, whole chunks of eight.
+template <int DT>
+bool few_ok(const Product& p) {
+  const int64_t a = 16 / bytes_of(DT);
+  return p.K % 8 == 0 && aligned(p.A.p, 16) && aligned(p.B.p, 16) && p.A.ld % a == 0 && p.B.ld % a == 0 &&
+         std::max(p.A.ld, p.B.ld) <= kFastLd / 2;
+}
+
 // How a product is run: over `splits` parts of k, `per` steps each (the last may have fewer), whose sums are joined.
 enum Form { kAny, kSmall, kLarge };  // k_linear_any, k_linear_bf16 of 128 x 128, of 256 x 256
 struct Plan {
@@ -167,12 +175,12 @@ int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
     if (ws_bytes < need) return EF_EWORKSPACE;
   }
   const bool fast = DT == EF_BF16 && fast_ok<KIND>(p);
-  if constexpr (KIND == K_FWD && DT == EF_BF16) {
-    if (fast && p.M <= kFewTokens) {
+  if constexpr (KIND == K_FWD) {
+    if (p.M <= kFewTokens && few_ok<DT>(p)) {
       // (32 outputs a workgroup where a group of the checkpoint needs them, or where half the workgroups fill the CUs)
       const int ot = p.ep.k.codes || p.N >= 16 * 4 * kCUs ? 2 : 1;
       const dim3 grid((unsigned)((p.N + 16 * ot - 1) / (16 * ot))), blk(kFewWaves * 64);
-#define EF_FEW(TT, OT) EF_LAUNCH_AS("k_linear_few forward", (k_linear_few<TT, OT>), grid, blk, 0, st, (int32_t)p.M, (int32_t)p.N, (int32_t)p.K, p.A, p.B, p.ep)
+#define EF_FEW(TT, OT) EF_LAUNCH_AS("k_linear_few forward", (k_linear_few<DT, TT, OT>), grid, blk, 0, st, (int32_t)p.M, (int32_t)p.N, (int32_t)p.K, p.A, p.B, p.ep)
       if (p.M <= 16 && ot == 1) EF_FEW(1, 1);
       else if (p.M <= 16) EF_FEW(1, 2);
       else if (ot == 1) EF_FEW(2, 1);

@@ -734,3 +734,21 @@ def test_two_streams_at_once_and_twice_the_same():
             e.ef_linear_wgrad(dy, q, s, 0, dw[k], wsp[k], stream=side[k])
         torch.cuda.synchronize()
         assert torch.equal(dw[0], dw[2]) and torch.equal(dw[1], dw[2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,i,o", [(1, 4096, 1000), (3, 264, 16), (16, 1032, 40), (17, 8, 4100), (32, 520, 33), (33, 520, 33), (2, 36, 50)])
+def test_few_tokens_of_integers_bit_for_bit(n, i, o, dtype):
+    import torch
+    for k in range(2):  # contiguous rows, padded rows
+        announce("few ints", n, i, o, dtype, k)
+        rng = np.random.default_rng([n, i, o, k])
+        x, w, b, r = ints(rng, n, i), ints(rng, o, i), ints(rng, 1, o)[0], ints(rng, n, o)
+        z = x @ w.T + b
+        for keep in (False, True):
+            y, q, s = forward(x, w, b, r, dtype, L.RELU, keep, k, k)
+            assert np.array_equal(val(y), torch.from_numpy(np.maximum(z, 0) + r).to(tt(dtype)).double().numpy())
+        wq, wsc = L.ckpt_pack(z, k)
+        assert np.array_equal(host(s), wsc)
+        neg0 = 0 if k == L.INT8 else 128
+        assert np.array_equal(np.where(host(q) == neg0, 0, host(q)), np.where(wq == neg0, 0, wq))

@@ -417,11 +417,14 @@ size_t ef_workspace_diag_offset(const ef_layout* layout, int op);
  *    rows) of at least their columns; any element-aligned address and any ld
  *    is taken (rows that start on 16 bytes are read fastest).  dtype is
  *    EF_F32 or EF_BF16, one for all matrices of a call.
- *  - Products and sums are held in float32 and rounded once, where they are
- *    stored.  The order of every sum is fixed by the sizes: results are
- *    bitwise reproducible.
- *  - Outputs must not overlap inputs, except where a call says so
- *    (EF_EINVAL).
+ *  - Sums are held in float32 and rounded once, where they are stored.  The
+ *    order of every sum is fixed by the sizes, the types and the alignment of
+ *    the matrices: the same call is bitwise reproducible.  float32 operands
+ *    are multiplied as sums of three bfloat16 numbers, each product to 2^-23
+ *    of itself; an infinity among them comes out as NaN, and magnitudes under
+ *    2^-110 lose digits.
+ *  - Outputs must not overlap inputs, other outputs or ws, except where a
+ *    call says so (EF_EINVAL; columns of one buffer side by side are fine).
  *  - ws: 256-byte aligned, at least ef_linear_workspace_bytes bytes (may be
  *    null where that is 0); contents need not be preserved. */
 int64_t ef_ckpt_row_bytes(int64_t c);

@@ -30,20 +30,28 @@ bool kept_ok(const uint8_t* codes, const uint8_t* scales, int64_t rows) {
   return rows == 0 || (codes && scales && aligned(codes, 16));
 }
 
+// The bytes of a matrix: from a to b, `width` of every `stride`.
 struct Range {
   const char *a, *b;
+  int64_t stride, width;
 };
 Range range(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t size) {
   const char* q = static_cast<const char*>(p);
-  if (!q || !rows) return {nullptr, nullptr};
-  return {q, q + ((rows - 1) * ld + cols) * size};
+  if (!q || !rows) return {nullptr, nullptr, 0, 0};
+  return {q, q + ((rows - 1) * ld + cols) * size, ld * size, cols * size};
 }
 Range range_kept(const uint8_t* codes, int64_t rows, int64_t c) {
   const int64_t row = (int64_t)groups(c) * kGroup;
   return range(codes, rows, row, row, 1);
 }
 Range range_scales(const uint8_t* s, int64_t rows, int64_t c) { return range(s, rows, groups(c), groups(c), 1); }
-bool meet(Range x, Range y) { return x.a < y.b && y.a < x.b; }
+bool meet(Range x, Range y) {
+  if (!(x.a < y.b && y.a < x.b)) return false;
+  if (x.stride != y.stride) return true;
+  // rows equally far apart: side by side in the same rows (columns of one buffer) they do not meet
+  const int64_t d = ((y.a - x.a) % x.stride + x.stride) % x.stride;
+  return d < x.width || d + y.width > x.stride;
+}
 template <typename... R> bool meet_any(Range x, R... y) { return (meet(x, y) || ...); }
 
 // Grid of the elementwise passes: lanes per row (as a power of two's exponent), rows and columns of workgroups.
@@ -302,8 +310,8 @@ int ef_linear_forward(int64_t n, int64_t i, int64_t o, const void* x, int64_t ld
   const int64_t b = bytes_of(dtype);
   const Range out = range(y, n, o, ldy, b), rx = range(x, n, i, ldx, b), rw = range(w, o, i, ldw, b),
               rb = range(bias, 1, o, o, b), rr = range(res, n, o, ldr, b),
-              q = codes ? range_kept(codes, n, o) : Range{nullptr, nullptr},
-              s = codes ? range_scales(scales, n, o) : Range{nullptr, nullptr};
+              q = codes ? range_kept(codes, n, o) : Range{nullptr, nullptr, 0, 0},
+              s = codes ? range_scales(scales, n, o) : Range{nullptr, nullptr, 0, 0};
   if (meet_any(out, rx, rw, rb, q, s) || meet_any(q, s, rx, rw, rb, rr) || meet_any(s, rx, rw, rb, rr)) return EF_EINVAL;
   if (meet(out, rr) && !(res == y && ldr == ldy)) return EF_EINVAL;
   if (n == 0) return EF_OK;

@@ -752,3 +752,24 @@ def test_few_tokens_of_integers_bit_for_bit(n, i, o, dtype):
         assert np.array_equal(host(s), wsc)
         neg0 = 0 if k == L.INT8 else 128
         assert np.array_equal(np.where(host(q) == neg0, 0, host(q)), np.where(wq == neg0, 0, wq))
+
+
+def test_columns_of_one_buffer():
+    """Inputs and outputs side by side in the rows of one buffer, as slices of its columns."""
+    import torch
+    e = E()
+    n, i, o = 96, 64, 128
+    x, w, r = gpu_ints(1, n, i), gpu_ints(2, o, i), gpu_ints(3, n, o)
+    for dtype in ("f32", "bf16"):
+        t = tt(dtype)
+        buf = torch.zeros(n, i + 2 * o + 8, dtype=t, device="cuda")
+        a, y, res = buf[:, :i], buf[:, i:i + o], buf[:, i + o:i + 2 * o]
+        a.copy_(x), res.copy_(r)
+        wk = ws(e.EF_OP_FORWARD, n, i, o, dtype)
+        e.ef_linear_forward(a, w.to(t), y, wk, act=L.RELU, res=res)
+        assert torch.equal(y, (mm64(x, w.t()).clamp(min=0) + r).to(t))
+        assert torch.equal(a, x.to(t)) and torch.equal(res, r.to(t)) and not buf[:, i + 2 * o:].any()
+        with pytest.raises(e.EfError):
+            e.ef_linear_forward(a, w.to(t), buf[:, i - 1:i - 1 + o], wk)
+        with pytest.raises(e.EfError):
+            e.ef_linear_forward(a, w.to(t), y, wk, res=buf[:, i + 1:i + 1 + o])

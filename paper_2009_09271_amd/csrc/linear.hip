@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 using namespace efs;
 
@@ -176,11 +177,14 @@ constexpr const char* kLabel[4][3] = {
     {"k_linear_join forward", "k_linear_join dgrad", "k_linear_join wgrad"}};
 
 template <int KIND, int DT, int DO>
-int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st) {
+int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st, std::initializer_list<Range> others) {
   const size_t need = product_bytes(KIND == K_WGRAD, DT, p.M, p.N, p.K);
   if (need) {
     if (!ws || !aligned(ws, kAlign)) return EF_EINVAL;
     if (ws_bytes < need) return EF_EWORKSPACE;
+    const Range r = range(ws, 1, (int64_t)need, (int64_t)need, 1);
+    for (const Range& x : others)
+      if (meet(r, x)) return EF_EINVAL;
   }
   const bool fast = DT == EF_BF16 && fast_ok<KIND>(p);
   if constexpr (KIND == K_FWD) {
@@ -316,8 +320,8 @@ int ef_linear_forward(int64_t n, int64_t i, int64_t o, const void* x, int64_t ld
   if (meet(out, rr) && !(res == y && ldr == ldy)) return EF_EINVAL;
   if (n == 0) return EF_OK;
   Product p{n, o, i, {x, ldx}, {w, ldw}, {}, {y, ldy, bias, res, ldr, {codes, scales, groups(o), fmt}, act, 0, nullptr}};
-  return dtype == EF_F32 ? run_product<K_FWD, EF_F32, EF_F32>(p, ws, ws_bytes, S(stream))
-                         : run_product<K_FWD, EF_BF16, EF_BF16>(p, ws, ws_bytes, S(stream));
+  return dtype == EF_F32 ? run_product<K_FWD, EF_F32, EF_F32>(p, ws, ws_bytes, S(stream), {out, rx, rw, rb, rr, q, s})
+                         : run_product<K_FWD, EF_BF16, EF_BF16>(p, ws, ws_bytes, S(stream), {out, rx, rw, rb, rr, q, s});
 }
 
 int ef_linear_dgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t lddy, const void* w, int64_t ldw, int act,
@@ -330,15 +334,16 @@ int ef_linear_dgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t ldd
   const bool kept = act != EF_ACT_NONE;
   if (kept && (!fmt_ok(fmt) || !kept_ok(codes, scales, n))) return EF_EINVAL;
   const int64_t b = bytes_of(dtype);
-  const Range out = range(dx, n, i, lddx, b), rr = range(res, n, i, ldr, b);
-  if (meet_any(out, range(dy, n, o, lddy, b), range(w, o, i, ldw, b))) return EF_EINVAL;
-  if (kept && meet_any(out, range_kept(codes, n, i), range_scales(scales, n, i))) return EF_EINVAL;
+  const Range out = range(dx, n, i, lddx, b), rr = range(res, n, i, ldr, b), ry = range(dy, n, o, lddy, b),
+              rw = range(w, o, i, ldw, b), q = kept ? range_kept(codes, n, i) : Range{nullptr, nullptr, 0, 0},
+              s = kept ? range_scales(scales, n, i) : Range{nullptr, nullptr, 0, 0};
+  if (meet_any(out, ry, rw, q, s)) return EF_EINVAL;
   if (meet(out, rr) && !(res == dx && ldr == lddx)) return EF_EINVAL;
   if (n == 0) return EF_OK;
   Product p{n, i, o, {dy, lddy}, {w, ldw}, {},
             {dx, lddx, nullptr, res, ldr, {const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), groups(i), fmt}, act, 0, nullptr}};
-  return dtype == EF_F32 ? run_product<K_DGRAD, EF_F32, EF_F32>(p, ws, ws_bytes, S(stream))
-                         : run_product<K_DGRAD, EF_BF16, EF_BF16>(p, ws, ws_bytes, S(stream));
+  return dtype == EF_F32 ? run_product<K_DGRAD, EF_F32, EF_F32>(p, ws, ws_bytes, S(stream), {out, ry, rw, rr, q, s})
+                         : run_product<K_DGRAD, EF_BF16, EF_BF16>(p, ws, ws_bytes, S(stream), {out, ry, rw, rr, q, s});
 }
 
 int ef_linear_wgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t lddy, int dtype, const uint8_t* codes,
@@ -357,10 +362,10 @@ int ef_linear_wgrad(int64_t n, int64_t i, int64_t o, const void* dy, int64_t ldd
   Product p{o, i, n, {dy, lddy}, {}, {const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), groups(i), fmt},
             {dw, i, nullptr, nullptr, 0, {}, EF_ACT_NONE, accumulate ? 1 : 0, db}};
   if (dtype == EF_F32)
-    return g_dtype == EF_F32 ? run_product<K_WGRAD, EF_F32, EF_F32>(p, ws, ws_bytes, st)
-                             : run_product<K_WGRAD, EF_F32, EF_BF16>(p, ws, ws_bytes, st);
-  return g_dtype == EF_F32 ? run_product<K_WGRAD, EF_BF16, EF_F32>(p, ws, ws_bytes, st)
-                           : run_product<K_WGRAD, EF_BF16, EF_BF16>(p, ws, ws_bytes, st);
+    return g_dtype == EF_F32 ? run_product<K_WGRAD, EF_F32, EF_F32>(p, ws, ws_bytes, st, {rw, rb, ry, q, s})
+                             : run_product<K_WGRAD, EF_F32, EF_BF16>(p, ws, ws_bytes, st, {rw, rb, ry, q, s});
+  return g_dtype == EF_F32 ? run_product<K_WGRAD, EF_BF16, EF_F32>(p, ws, ws_bytes, st, {rw, rb, ry, q, s})
+                           : run_product<K_WGRAD, EF_BF16, EF_BF16>(p, ws, ws_bytes, st, {rw, rb, ry, q, s});
 }
 
 }  // extern "C"

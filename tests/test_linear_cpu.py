@@ -158,6 +158,22 @@ def test_products_refuse():
         assert wgr(**bad) == E.EF_EINVAL, bad
 
 
+def test_products_refuse_a_workspace_over_their_matrices():
+    lib, n = E.lib(), 64
+    for op in (E.EF_OP_FORWARD, E.EF_OP_DGRAD):
+        assert lib.ef_linear_workspace_bytes(op, n, 8192, 8192, E.EF_BF16) > 0
+    assert lib.ef_linear_workspace_bytes(E.EF_OP_WGRAD, 8192, 64, 64, E.EF_BF16) > 0
+    size = 1 << 40
+    for over in range(7):  # (at(k): the k-th buffer of the call, the workspace laid over it from its start)
+        forward = lib.ef_linear_forward(n, 8192, 8192, at(0), 8192, at(1), 8192, at(2), 0, at(3), 8192, at(4), 8192, E.EF_BF16,
+                                        at(5), at(6), 0, at(over), size, None)
+        dgrad = lib.ef_linear_dgrad(n, 8192, 8192, at(0), 8192, at(1), 8192, 1, at(2), at(3), 0, at(4), 8192, at(5), 8192,
+                                    E.EF_BF16, at(min(over, 5)), size, None)
+        wgrad = lib.ef_linear_wgrad(8192, 64, 64, at(0), 64, E.EF_BF16, at(1), at(2), 0, at(3), at(4), E.EF_F32, 0,
+                                    at(min(over, 4)), size, None)
+        assert (forward, dgrad, wgrad) == (E.EF_EINVAL,) * 3, over
+
+
 def test_binding_refuses_what_does_not_fit():
     import torch
     x, w, y = torch.zeros(4, 8), torch.zeros(40, 8), torch.zeros(4, 40)

@@ -412,7 +412,9 @@ size_t ef_workspace_diag_offset(const ef_layout* layout, int op);
  * Shared by these calls:
  *  - n tokens (rows; 0 is allowed and does nothing, or gives a gradient of
  *    zeros), i input and o output features; 0 <= n < 2^31, 1 <= i, c, o
- *    <= 2^26, else EF_ERANGE.
+ *    <= 2^26, and a product's result of less than about 2^38 elements (its
+ *    tiles of 128 x 128, or 256 x 256, are launched as less than 2^32
+ *    threads), else EF_ERANGE.
  *  - Matrices are row-major with a leading dimension ld (elements between
  *    rows) of at least their columns; any element-aligned address and any ld
  *    is taken (rows that start on 16 bytes are read fastest).  dtype is

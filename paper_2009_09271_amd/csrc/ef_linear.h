@@ -326,7 +326,7 @@ struct Kept {
 template <int DT>
 __global__ __launch_bounds__(256) void k_ckpt_pack(int64_t n, int32_t c, const void* x, int64_t ldx, Kept k, int txs) {
   const int tx = threadIdx.x & ((1 << txs) - 1), ty = threadIdx.x >> txs;
-  const int64_t row = (int64_t)blockIdx.x * (256 >> txs) + ty;
+  const int64_t row = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * (256 >> txs) + ty;
   const int32_t col = ((int32_t)(blockIdx.y << txs) + tx) * 8;
   if (row >= n || col >= k.G * kGroup) return;  // (whole groups: 4 lanes, 32 columns)
   Raw<DT> raw;
@@ -344,7 +344,7 @@ template <int DT, bool ACT>
 __global__ __launch_bounds__(256) void k_ckpt_unpack(int64_t n, int32_t c, int act, Kept k, const void* dy, int64_t lddy, void* y,
                                                      int64_t ldy, int txs) {
   const int tx = threadIdx.x & ((1 << txs) - 1), ty = threadIdx.x >> txs;
-  const int64_t row = (int64_t)blockIdx.x * (256 >> txs) + ty;
+  const int64_t row = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * (256 >> txs) + ty;
   const int32_t col = ((int32_t)(blockIdx.y << txs) + tx) * 8;
   if (row >= n || col >= c) return;
   const u32x2* from = reinterpret_cast<const u32x2*>(k.codes + row * k.G * kGroup + col);

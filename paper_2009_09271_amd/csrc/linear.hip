@@ -14,7 +14,7 @@ namespace {
 
 constexpr int64_t kMaxWidth = (int64_t)1 << 26;  // columns, and output features
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
-constexpr int64_t kMaxGrid = 0x7FFFFFFF;
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;  // of a grid, along one dimension
 
 bool dtype_ok(int t) { return t == EF_F32 || t == EF_BF16; }
 bool fmt_ok(int f) { return f == EF_CKPT_INT8 || f == EF_CKPT_E4M3; }
@@ -55,7 +55,8 @@ bool meet(Range x, Range y) {
 }
 template <typename... R> bool meet_any(Range x, R... y) { return (meet(x, y) || ...); }
 
-// Grid of the elementwise passes: lanes per row (as a power of two's exponent), rows and columns of workgroups.
+// Grid of the elementwise passes: lanes per row (as a power of two's exponent), and workgroups: columns along y, rows
+// along x and, from 2^23 on, z.
 struct Flat {
   dim3 grid;
   int txs;
@@ -65,8 +66,9 @@ int flat_of(int64_t n, int64_t c, Flat* f) {
   int txs = 2;
   while (txs < 8 && ((int64_t)1 << txs) < lanes) ++txs;
   const int64_t gx = (n + (256 >> txs) - 1) / (256 >> txs), gy = (lanes + ((int64_t)1 << txs) - 1) >> txs;
-  if (gx > kMaxGrid || gy > 65535) return EF_ERANGE;
-  f->grid = dim3((unsigned)gx, (unsigned)gy);
+  const int64_t most = (int64_t)1 << 23, gz = (gx + most - 1) / most;
+  if (gz > 65535 || gy > 65535) return EF_ERANGE;
+  f->grid = dim3((unsigned)std::min(gx, most), (unsigned)gy, (unsigned)gz);
   f->txs = txs;
   return EF_OK;
 }
@@ -203,7 +205,7 @@ int run_product(const Product& p, void* ws, size_t ws_bytes, hipStream_t st, std
   }
   const Plan pl = plan_of(fast, KIND == K_WGRAD, DT == EF_F32, p.M, p.N, p.K);
   const int64_t tile = pl.form == kLarge ? 256 : 128, tiles = ((p.M + tile - 1) / tile) * ((p.N + tile - 1) / tile);
-  if (tiles * pl.splits > kMaxGrid) return EF_ERANGE;
+  if (tiles * pl.splits > kMaxThreads / (pl.form == kLarge ? 512 : 256)) return EF_ERANGE;
   Split sp{nullptr, nullptr, p.M * padded(p.N), padded(p.N), pl.per, pl.splits};
   if (pl.splits > 1) {
     sp.part = static_cast<float*>(ws);

@@ -773,3 +773,18 @@ def test_columns_of_one_buffer():
             e.ef_linear_forward(a, w.to(t), buf[:, i - 1:i - 1 + o], wk)
         with pytest.raises(e.EfError):
             e.ef_linear_forward(a, w.to(t), y, wk, res=buf[:, i + 1:i + 1 + o])
+
+
+def test_passes_over_more_rows_than_one_grid_dimension_has():
+    """2^32 threads and more: 2^30 rows of one group each."""
+    import torch
+    e, n = E(), (1 << 30) + 100
+    announce("passes over", n, "rows")
+    x = torch.arange(n, device="cuda", dtype=torch.int32).remainder_(15).sub_(7).to(torch.bfloat16).unsqueeze(1)
+    q, s = e.ckpt_buffers(n, 1)
+    e.ef_ckpt_pack(x, q, s)
+    y = torch.empty_like(x)
+    e.ef_ckpt_unpack(q, s, L.INT8, y)
+    assert torch.equal(x, y)
+    e.ef_ckpt_act_backward(L.RELU, q, s, L.INT8, x, y)
+    assert torch.equal(x.clamp_(min=0), y)

@@ -174,6 +174,17 @@ def test_products_refuse_a_workspace_over_their_matrices():
         assert (forward, dgrad, wgrad) == (E.EF_EINVAL,) * 3, over
 
 
+def test_products_refuse_more_tiles_than_a_grid_has():
+    """A grid has less than 2^32 threads: 2^24 tiles of 128 x 128 or 2^23 of 256 x 256 are too many."""
+    lib, n = E.lib(), (1 << 31) - 1
+    far = [P(1 << (48 + k)) for k in range(5)]
+    for dt, i, o in ((E.EF_F32, 1, 1), (E.EF_BF16, 1, 1), (E.EF_BF16, 8, 264)):
+        assert lib.ef_linear_forward(n, i, o, far[0], i, far[1], i, None, 0, None, 0, far[2], o, dt, None, None, 0, far[3], 1 << 60,
+                                     None) == E.EF_ERANGE
+        assert lib.ef_linear_dgrad(n, o, i, far[0], i, far[1], o, 0, None, None, 0, None, 0, far[2], o, dt, far[3], 1 << 60,
+                                   None) == E.EF_ERANGE
+
+
 def test_binding_refuses_what_does_not_fit():
     import torch
     x, w, y = torch.zeros(4, 8), torch.zeros(40, 8), torch.zeros(4, 40)

@@ -548,17 +548,28 @@ struct Mat {
 //   dgrad    A = dy [n][o] (k along the row), B = W [o][i] (k down the rows)
 //   wgrad    A = dy [t][o] (k down the rows), B = the checkpoint [t][i] (k down the rows)
 //
-// k_linear_bf16, for bfloat16 matrices whose rows start on 16 bytes.  A workgroup has BM x BN of C, WM x WN wavefronts, and steps of 64 along k through two halves of the LDS.  A
-// wavefront has BM / WM rows and 64 columns of C in accumulators of 32 x 32.  Operands go from memory to the LDS
-// without passing registers (16 bytes a lane; what lies outside the matrix arrives as zeros by the buffer's
-// bounds), in the order that they have in memory:
+// k_linear_bf16, for bfloat16 matrices whose rows start on 16 bytes.  A workgroup has BM x BN of C, WM x WN wavefronts,
+// and steps of 64 along k; a wavefront has BM / WM rows and 64 columns of C in accumulators of 32 x 32.  A's tiles take
+// turns in three parts of the LDS, B's in two: 256 x 256 fills its 160 KB, one workgroup a CU, and 128 x 128 half of it,
+// two a CU.  Operands go from memory to the LDS without passing registers (16 bytes a lane; what lies outside the matrix
+// arrives as zeros by the buffer's bounds), in the order that they have in memory:
 //   k along the row   [line][64]: 16-byte chunk c of line r at place c ^ (r >> 1 & 7), so that sixteen lines' reads
 //                     of one k fall on different banks (two lines span them all); read 16 bytes a lane
 //   k down the rows   [64][line]: 64-byte unit u of row k at place u ^ (k & 3), so that four rows' reads do; read
 //                     by the transposing load, which hands four k of one line to a lane
 //   checkpoint        as k down the rows: its codes pass through registers, where they become bfloat16
-// A step's last fragments are read before the barrier that releases its half, and the next step's first ones
-// after it, ahead of the last fragments' instructions: the matrix pipes have work while the LDS changes hands.
+// A step's last fragments are read before the barrier that releases its parts, and the next step's first ones
+// after it, among the last fragments' instructions: the matrix pipes have work while the LDS changes hands.
+//
+// What bounds it: the matrix instructions, and the chip's power under them (1.5 to 1.7 GHz while they run).  Kernel
+// times of n, i, o, and the share of the cycles in which the matrix pipes work:
+//   forward 8192, 4096, 16384, GELU and checkpoint  970 us, 1.13 PFLOP/s, 68 % (the loop alone 93 %; the epilogue takes
+//           34 thousand cycles of a tile's 191, the start 18)
+//   dgrad   8192, 4096, 4096, GELU                  248 to 260 us, 1.1 PFLOP/s, 64 %
+//   wgrad   8192, 4096, 16384                       1005 us, 1.09 PFLOP/s, 61 % (decoding the codes)
+//   forward 4096, 768, 768 on 128 x 128 tiles       13 to 15 us, 192 workgroups, 12 steps: mostly start and epilogue
+// Tried: four wavefronts of 128 x 128 on 256 x 256 (1788 thousand cycles against 1531), the L2 warmed a step ahead (1789
+// against 1687 then), a fourth part for the 128 x 128 tiles' operands (14.8 us against 12.4).
 // ---------------------------------------------------------------------------------------------
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -583,7 +594,7 @@ constexpr int64_t kFastLd = (int64_t)1 << 21;  // leading dimensions up to this 
 #endif
 
 // 16 bytes a lane from offset `off` of a buffer to the LDS, the lanes side by side from lds on; what lies outside the
-// buffer arrives as zeros.  Written out: the compiler, which cannot tell the two halves of the LDS apart, would let
+// buffer arrives as zeros.  Written out: the compiler, which cannot tell the parts of the LDS apart, would let
 // later reads of the LDS wait for it.  It has no result register; the wait before the barrier covers it.
 __device__ __forceinline__ void buffer_to_lds(const char* base, uint32_t bytes, const char* lds, int off) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -798,8 +809,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
   for (int a = 0; a < TM; ++a) bs[a] = 0.0f;
   bf16x8 fa[2][TM], fb[2][TN];
   // One slice: the matrix instructions of the fragments h, and between them, one by one, the reads of the next ones
-  // (slice ks of the tiles from_a and from_b, where there are `more`) and whatever else there is to do.  Pinned in this order: left to itself the compiler gathers the
-  // reads before their use.
+  // (slice ks of the tiles from_a and from_b, where there are `more`) and whatever else there is to do.  Pinned in this
+  // order: left to itself the compiler gathers the reads before their use.
   constexpr int kMul = TM * TN;
   auto slice = [&](auto more, int h, const char* from_a, const char* from_b, int ks, auto&& between) {
 #pragma unroll
@@ -1180,8 +1191,9 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
 // The forward product of a few tokens (up to 16 TT): the weights are read once, and that bounds it.  A workgroup
 // has 16 OT output features and splits k over its eight wavefronts; each takes the weights' rows as the first
 // operand and the tokens as the second, straight from memory to registers, 16 bytes a lane, eight loads of the
-// weights in flight (sixteen, or past the caches: no faster); float32 as in k_linear_any.  4096 x 4096 weights in bfloat16,
-// one token: 8.1 us, 4.2 TB/s, of which 3 us are the launch and the last loads' latency.  The eight partial sums are added in order through the LDS.
+// weights in flight (sixteen: 8.6 us against 8.1, past the caches 10.2); float32 as in k_linear_any.  4096 x 4096
+// weights in bfloat16, one token: 8.1 to 9 us, about 4 TB/s, of which 3 us are the launch and the last loads' latency.
+// The eight partial sums are added in order through the LDS.
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewWaves = 8;
 constexpr int kFewTokens = 32;

@@ -881,8 +881,11 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
     decode(codes[1], 0, 1, b1);
     sk.fetch(s0 + 2, codes[0]);
   }
-  __builtin_amdgcn_s_waitcnt(0);
-  __syncthreads();
+  // The first fragments wait for the first step's tiles alone (a checkpoint's codes have passed already): the barrier that
+  // ends it waits for the second's.  n, i, o = 4096, 768, 768: 14.6 -> 14.1 us.
+  if (B8) __builtin_amdgcn_s_waitcnt(0);
+  else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * SA::J) : "memory");
+  asm volatile("s_barrier" ::: "memory");
 #pragma unroll
   for (int t = 0; t < TM; ++t) fa[0][t] = ra.read(a0, 0, t);
 #pragma unroll

@@ -1033,13 +1033,14 @@ struct Chunks {
       p[j] = static_cast<const char*>(m.p) + (KC ? l * ld + k * S : k * ld + l * S);
     }
   }
-  // left: k from this step's first on
+  // left: k from this step's first on; WHOLE: more than the step's, and rows that are not narrow
+  template <bool WHOLE>
   __device__ __forceinline__ void fetch(int set, int64_t left, int t) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int64_t mine = left - At::k(t, j);
       int n = 8;
-      if (left <= kAnyK || narrow) n = KC ? (mine < 8 ? (int)mine : 8) : (mine > 0 ? cnt : 0);
+      if (!WHOLE && (left <= kAnyK || narrow)) n = KC ? (mine < 8 ? (int)mine : 8) : (mine > 0 ? cnt : 0);
       raw[set][j].load(p[j], 0, n);
       p[j] += step;
     }
@@ -1080,12 +1081,13 @@ struct KeptChunks {
       s[j] = m.scales + (k0 + At::k(t, j)) * m.G + l / kGroup;
     }
   }
+  template <bool WHOLE>
   __device__ __forceinline__ void fetch(int set, int64_t left, int t) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       code[set][j] = u32x2{0u, 0u};
       scale[set][j] = 0u;
-      if (left >= kAnyK || At::k(t, j) < left) {
+      if (WHOLE || At::k(t, j) < left) {
         code[set][j] = *reinterpret_cast<const u32x2*>(q[j]);
         scale[set][j] = *s[j];
       }
@@ -1137,19 +1139,21 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
   ca.init(A, m0, M, s0 * kAnyK, t);
   if (B8) ck.init(BK, n0, s0 * kAnyK, t);
   else cb.init(B, n0, N, s0 * kAnyK, t);
-  auto fetch = [&](int64_t s, int set) {
+  auto fetch = [&](auto whole, int64_t s, int set) {
+    constexpr bool W = decltype(whole)::value;
     const int64_t left = K - s * kAnyK;
-    ca.fetch(set, left, t);
-    if (B8) ck.fetch(set, left, t);
-    else cb.fetch(set, left, t);
+    ca.template fetch<W>(set, left, t);
+    if (B8) ck.template fetch<W>(set, left, t);
+    else cb.template fetch<W>(set, left, t);
   };
-  auto step = [&](int64_t s, int set) {
+  auto step = [&](auto whole, int64_t s, int set) {
+    __builtin_amdgcn_sched_barrier(0);  // (nothing of this step into the one before it: its loads would be waited for there)
     __syncthreads();
     ca.put(set, lds, t);
     if (B8) ck.put(set, lds + PA * kPlane, BK.fmt, t);
     else cb.put(set, lds + PA * kPlane, t);
     __syncthreads();
-    if (s + 2 < s1) fetch(s + 2, set);
+    if (decltype(whole)::value || s + 2 < s1) fetch(whole, s + 2, set);
 #pragma unroll
     for (int ks = 0; ks < kAnyK / 16; ++ks) {
       bf16x8 fa[PA][2], fb[PB][2];
@@ -1179,11 +1183,26 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
       }
     }
   };
-  if (s0 < s1) fetch(s0, 0);
-  if (s0 + 1 < s1) fetch(s0 + 1, 1);
-  for (int64_t s = s0; s < s1; s += 2) {
-    step(s, 0);
-    if (s + 1 < s1) step(s + 1, 1);
+  // The steps whose chunks are whole (all but the last one) in a loop without branches: where some lanes load elements
+  // and others chunks, the compiler waits for everything that is under way, and two steps ahead become one.  (float32,
+  // dgrad of 8192, 4096, 1024: 393 -> 371 us, 1.1 PFLOP/s in bfloat16 products; 4096, 768, 768 forward: 38.5 -> 36.5.)
+  const bool narrow = ca.narrow || (!B8 && cb.narrow);
+  const int64_t whole = narrow ? s0 : s1 < all ? s1 : all - 1;
+  int64_t s = s0;
+  if (s0 + 3 < whole) {
+    fetch(std::true_type{}, s0, 0);
+    fetch(std::true_type{}, s0 + 1, 1);
+    for (; s + 3 < whole; s += 2) {
+      step(std::true_type{}, s, 0);
+      step(std::true_type{}, s + 1, 1);
+    }
+  } else {
+    if (s0 < s1) fetch(std::false_type{}, s0, 0);
+    if (s0 + 1 < s1) fetch(std::false_type{}, s0 + 1, 1);
+  }
+  for (; s < s1; s += 2) {
+    step(std::false_type{}, s, 0);
+    if (s + 1 < s1) step(std::false_type{}, s + 1, 1);
   }
   __syncthreads();
   finish<KIND, DO, 2, 1>(acc, lds, wave, lane, m0 + wm, n0 + wn, M, N, ep, sp, my.z);

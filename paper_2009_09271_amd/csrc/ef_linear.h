@@ -563,10 +563,10 @@ struct Mat {
 //
 // What bounds it: the matrix instructions, and the chip's power under them (1.5 to 1.7 GHz while they run).  Kernel
 // times of n, i, o, and the share of the cycles in which the matrix pipes work:
-//   forward 8192, 4096, 16384, GELU and checkpoint  970 us, 1.13 PFLOP/s, 68 % (the loop alone 93 %; the epilogue takes
-//           34 thousand cycles of a tile's 191, the start 18)
-//   dgrad   8192, 4096, 4096, GELU                  248 to 260 us, 1.1 PFLOP/s, 64 %
-//   wgrad   8192, 4096, 16384                       1005 us, 1.09 PFLOP/s, 61 % (decoding the codes)
+//   forward 8192, 4096, 16384, GELU and checkpoint  945 to 970 us, 1.15 PFLOP/s, 67 % (the loop alone 93 %; the epilogue
+//           takes 34 thousand cycles of a tile's 191, the start 18)
+//   dgrad   8192, 4096, 4096, GELU                  243 to 260 us, 1.1 PFLOP/s, 65 %
+//   wgrad   8192, 4096, 16384                       965 to 1005 us, 1.1 PFLOP/s, 60 % (decoding the codes)
 //   forward 4096, 768, 768 on 128 x 128 tiles       13 to 15 us, 192 workgroups, 12 steps: mostly start and epilogue
 // Tried: four wavefronts of 128 x 128 on 256 x 256 (1788 thousand cycles against 1531), the L2 warmed a step ahead (1789
 // against 1687 then), a fourth part for the 128 x 128 tiles' operands (14.8 us against 12.4).
@@ -662,7 +662,9 @@ struct Stream {
 };
 
 // A checkpoint's way: NT threads, LINES columns per tile; a thread has J chunks of sixteen codes, half a group each,
-// in registers, and passes them on as bfloat16 in quarters of a step.
+// in registers, and passes them on as bfloat16 in quarters of a step.  (Neighbours write 32 bytes apart: a fifth of the
+// LDS's cycles are bank conflicts, and hide.  Halves in turns, which leaves none: 998 -> 1028 us with loads of half the
+// size, 1045 with selects, wgrad of 8192, 4096, 16384.)
 template <int FMT, int LINES, int NT>
 struct StreamKept {
   static constexpr int J = kBK * LINES / 16 / NT;
@@ -967,7 +969,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
 // nothing of its 24 bits.  Of the nine products of two such sums the six that matter are taken; what is left out is
 // 2^-23 of the product at most.  A checkpoint's values are bfloat16 numbers, so against them three products are the
 // whole.  (Against the matrix instructions for float32, a sixteenth as fast: n, i, o = 1021, 771, 1285, dgrad
-// 49 -> 34 us; 2043, 1285, 771, wgrad 87 -> 36 us, each with its join.)  An infinity has no such parts: it comes out as NaN.
+// 49 -> 44 us, and 31 with the steps since; 2043, 1285, 771, wgrad 87 -> 38 us, and 35; each with its join.)  An infinity has no such parts: it comes out as NaN.
 // A workgroup has 128 x 128 of C, four wavefronts of 64 x 64.
 // ---------------------------------------------------------------------------------------------
 constexpr int kAnyTile = 128, kAnyK = 32;

@@ -717,6 +717,7 @@ struct StreamKept {
       b *= r;
       return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);  // (exact: the low halves are zeros)
     }
+    // (a scale of infinity gives NaN for every code: the conversion takes the scale's exponent, and the highest one for NaN)
     return __builtin_bit_cast(uint32_t, h & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, r, true)
                                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, r, false));
   }

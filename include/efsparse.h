@@ -402,12 +402,14 @@ size_t ef_workspace_diag_offset(const ef_layout* layout, int op);
  * Columns [32 g, 32 g + 32) of a row are a group with one power of two 2^e,
  * scales = e + 127: the smallest e >= -100 under which the group's largest
  * magnitude rounds to 127 or less (EF_CKPT_INT8) or is at most 448 * 2^e
- * (EF_CKPT_E4M3).  codes = value / 2^e rounded to nearest, ties to even;
- * the columns past c hold code 0.  A group with an infinity or a NaN has
- * scale 255 and codes 0 and stands for NaN, so an overflow stays visible in
- * every gradient that it reaches.  Decoded values code * 2^e are exact in
- * bfloat16.  Rows stand by themselves: rows [a, b) of a checkpoint are the
- * checkpoint of those rows.
+ * (EF_CKPT_E4M3).  codes = value / 2^e rounded to nearest, ties to even,
+ * and held at 63 under e = 122 (int8) and 240 under e = 120 (e4m3), whose
+ * next codes would stand for 2^128: a finite value comes back finite, there
+ * off by less than a step, else by half a step at most.  The columns past c
+ * hold code 0.  A group with an infinity or a NaN has scale 255 and codes 0
+ * and stands for NaN, so an overflow stays visible in every gradient that it
+ * reaches.  Decoded values code * 2^e are exact in bfloat16.  Rows stand by
+ * themselves: rows [a, b) of a checkpoint are the checkpoint of those rows.
  *
  * Shared by these calls:
  *  - n tokens (rows; 0 is allowed and does nothing, or gives a gradient of

@@ -22,6 +22,12 @@ def _fits(amax, e, fmt):
     return round(v) <= 127 if fmt == INT8 else v <= 448.0
 
 
+def _most(e, fmt):
+    """The largest code's value under 2^e that stands for a finite number (at most the largest bfloat16)."""
+    v = math.ldexp(float.fromhex("0x1.FEp127"), -e)
+    return min(127.0, math.floor(v)) if fmt == INT8 else float(_E4M3[_E4M3 <= v].max())
+
+
 def _group_exp(amax, fmt):
     e = max(LEAST_EXP, math.frexp(amax)[1] - 12) if amax > 0 else LEAST_EXP
     while not _fits(amax, e, fmt):
@@ -54,7 +60,7 @@ def ckpt_pack(x, fmt):
                 continue
             e = _group_exp(float(np.abs(v).max()), fmt)
             scales[r, g] = e + 127
-            s = np.ldexp(v, -e)
+            s = np.clip(np.ldexp(v, -e), -_most(e, fmt), _most(e, fmt)) if e > 100 else np.ldexp(v, -e)
             codes[r, g * GROUP:g * GROUP + len(v)] = (np.rint(s).astype(np.int64) & 255 if fmt == INT8 else _nearest_e4m3(s))
     return codes, scales
 

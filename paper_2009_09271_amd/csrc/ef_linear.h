@@ -3,7 +3,8 @@
 //
 // A checkpoint of x [n][c] is codes [n][32 G] and one scale byte per group of 32 columns of a row, G =
 // ceil(c / 32).  A group's scale is a power of two 2^e: the smallest (e >= kLeastExp) under which its largest
-// magnitude still fits the code, so no value saturates and each is off by at most half a step.  Powers of two
+// magnitude still fits the code, so each value is off by at most half a step (values that would round to 2^128 are held at
+// the largest finite code, off by less than a step).  Powers of two
 // make the decoded value code * 2^e exact in bfloat16 (at most seven significant bits, never subnormal), so the
 // matrix instructions take it as it is and a product with it rounds only where it sums.
 #pragma once
@@ -27,6 +28,10 @@ typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
 
 constexpr int kGroup = 32;       // columns that share a scale
 constexpr int kLeastExp = -100;  // smallest exponent of a group: 2^-100 times any code is a normal bfloat16
+// scale byte of the highest exponent of a group of finite values (122, 120), under which the codes 64 and 256 would stand for
+// 2^128, and the largest magnitude below, 63 * 2^122 and 240 * 2^120
+constexpr uint32_t kTopInt8 = 249, kTopE4m3 = 247;
+constexpr float kMostInt8 = 0x1.F8p127f, kMostE4m3 = 0x1.Ep127f;
 
 // ---------------------------------------------------------------------------------------------
 // Elements: eight neighbours of a row at a time.
@@ -155,9 +160,17 @@ __device__ __forceinline__ uint32_t group_scale(uint32_t amax, int fmt) {
 }
 
 // Eight codes of a group with scale byte s, in order from the low byte of [0].
-__device__ __forceinline__ u32x2 encode8(const float (&v)[8], uint32_t s, int fmt) {
+__device__ __forceinline__ u32x2 encode8(const float (&x)[8], uint32_t s, int fmt) {
   u32x2 q = {0u, 0u};
   if (s == 255u) return q;
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = x[j];
+  if (__builtin_expect(s >= kTopE4m3, 0)) {  // a finite value does not come back as an infinity
+    const float most = fmt == EF_CKPT_E4M3 ? kMostE4m3 : s == kTopInt8 ? kMostInt8 : 0x1.FFFFFEp127f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __builtin_amdgcn_fmed3f(v[j], -most, most);
+  }
   const float r = __uint_as_float((254u - s) << 23);  // 2^-e
 #pragma unroll
   for (int h = 0; h < 2; ++h) {

@@ -608,15 +608,19 @@ constexpr int64_t kFastLd = (int64_t)1 << 21;  // leading dimensions up to this 
 
 // 16 bytes a lane from offset `off` of a buffer to the LDS, the lanes side by side from lds on; what lies outside the
 // buffer arrives as zeros.  Written out: the compiler, which cannot tell the parts of the LDS apart, would let
-// later reads of the LDS wait for it.  It has no result register; the wait before the barrier covers it.
+// later reads of the LDS wait for it.  It has no result register; the wait before the barrier covers it.  (It overwrites m0,
+// which the compiler keeps for uses of its own and warns of; nothing else in these kernels has one.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void buffer_to_lds(const char* base, uint32_t bytes, const char* lds, int off) {
 #if defined(__HIP_DEVICE_COMPILE__)
   const uint64_t b = reinterpret_cast<uint64_t>(base);
   const u32x4 r = {(uint32_t)b, (uint32_t)(b >> 32), bytes, 0x00020000u};
   const uint32_t at = (uint32_t)reinterpret_cast<uintptr_t>((EF_LDS const char*)lds);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(r) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(r) : "memory", "m0");
 #endif
 }
+#pragma clang diagnostic pop
 
 // One operand's way into the LDS.  KC: k along the row.  LINES rows of C (or columns) per tile, NW wavefronts.
 // (K is at most 2^30 here: 32 bits hold every k.)

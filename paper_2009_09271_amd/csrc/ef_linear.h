@@ -884,7 +884,11 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
   }
   {
     const auto a = sa.aim(s0), a_next = sa.aim(s0 + 1);
-    const auto b = sb.aim(s0), b_next = sb.aim(s0 + 1);
+    typename SB::Aim b{}, b_next{};  // (a checkpoint has no Stream)
+    if constexpr (!B8) {
+      b = sb.aim(s0);
+      b_next = sb.aim(s0 + 1);
+    }
 #pragma unroll
     for (int j = 0; j < SA::J; ++j) {
       sa.load(j, a, a0, wave);
@@ -931,7 +935,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
     // This wavefront's part of the next step has arrived (all but the last loads, of A behind it), and its last reads
     // of this one.
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SA::J) : "memory");
-    const auto b = sb.aim(s + 2);
+    typename SB::Aim b{};
+    if constexpr (!B8) b = sb.aim(s + 2);
     slice(std::true_type{}, 1, a1, nxt, 0, [&](int i) {
       if (B8 && i == 0) sk.fetch(s + 3, now);
       if (!B8 && i % kGap == 0 && i / kGap < SB::J) sb.load(i / kGap, b, cur, wave);

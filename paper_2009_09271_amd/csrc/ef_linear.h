@@ -23,7 +23,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // the same at any address that an element may have: rows of odd lengths start anywhere
-typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(1)));
 typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
 
 constexpr int kGroup = 32;       // columns that share a scale

@@ -596,7 +596,7 @@ def linear_workspace(op, n, i, o, dtype, device="cuda"):
 def _ws(ws, where, dev):
     if ws is None:
         return 0, 0
-    if ws.get_device() != dev or not ws.is_contiguous():
+    if not isinstance(ws, _torch.Tensor) or ws.get_device() != dev or not ws.is_contiguous():
         raise EfError(EF_EINVAL, where, f"ws is not a contiguous tensor on cuda:{dev}")
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
@@ -644,7 +644,7 @@ def ef_linear_forward(x, weight, y, ws, bias=None, act=EF_ACT_NONE, res=None, co
         _vec(bias, "bias", w, dtypes, dev, o)
         b = bias.data_ptr()
     if res is not None:
-        r, ldr = res.data_ptr(), _mat(res, "res", w, dtypes, dev, n, o)
+        ldr, r = _mat(res, "res", w, dtypes, dev, n, o), res.data_ptr()
     if codes is not None or scales is not None:
         q, s = _kept(codes, scales, n, o, w, dev)
     _enqueue(_lib.ef_linear_forward, w, dev, stream, n, i, o, x.data_ptr(), ldx, weight.data_ptr(), ldw, b, act, r, ldr,
@@ -663,7 +663,7 @@ def ef_linear_dgrad(dy, weight, dx, ws, act=EF_ACT_NONE, codes=None, scales=None
     ldx = _mat(dx, "dx", w, dtypes, dev, n, i)
     r = ldr = q = s = 0
     if res is not None:
-        r, ldr = res.data_ptr(), _mat(res, "res", w, dtypes, dev, n, i)
+        ldr, r = _mat(res, "res", w, dtypes, dev, n, i), res.data_ptr()
     if act != EF_ACT_NONE:
         q, s = _kept(codes, scales, n, i, w, dev)
     _enqueue(_lib.ef_linear_dgrad, w, dev, stream, n, i, o, dy.data_ptr(), ldy, weight.data_ptr(), ldw, act, q, s, fmt, r, ldr,

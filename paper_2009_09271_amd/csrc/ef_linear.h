@@ -574,11 +574,12 @@ struct Mat {
 // after it, among the last fragments' instructions: the matrix pipes have work while the LDS changes hands.
 //
 // What bounds it: the matrix instructions, and the chip's power under them (1.5 to 1.7 GHz while they run).  Kernel
-// times of n, i, o, and the share of the cycles in which the matrix pipes work:
-//   forward 8192, 4096, 16384, GELU and checkpoint  945 to 970 us, 1.15 PFLOP/s, 67 % (the loop alone 93 %; the epilogue
+// times of n, i, o after a warm-up (the first 60 passes are up to 10 % slower), and the share of the cycles in which the
+// matrix pipes work:
+//   forward 8192, 4096, 16384, GELU and checkpoint  920 us, 1.19 PFLOP/s, 67 % (the loop alone 93 %; the epilogue
 //           takes 34 thousand cycles of a tile's 191, the start 18)
-//   dgrad   8192, 4096, 4096, GELU                  243 to 260 us, 1.1 PFLOP/s, 65 %
-//   wgrad   8192, 4096, 16384                       965 to 1005 us, 1.1 PFLOP/s, 60 % (decoding the codes)
+//   dgrad   8192, 4096, 4096, GELU                  241 to 250 us, 1.1 PFLOP/s, 65 %
+//   wgrad   8192, 4096, 16384                       970 to 1000 us, 1.1 PFLOP/s, 60 % (decoding the codes, and waits for them)
 //   forward 4096, 768, 768 on 128 x 128 tiles       13 to 15 us, 192 workgroups, 12 steps: mostly start and epilogue
 // Tried: four wavefronts of 128 x 128 on 256 x 256 (1788 thousand cycles against 1531), the L2 warmed a step ahead (1789
 // against 1687 then), a fourth part for the 128 x 128 tiles' operands (14.8 us against 12.4).
@@ -851,8 +852,10 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_bf16(int32_t M, int32
   // fragments' instructions (slice 3) are to be issued, and its parts of the LDS are free: for step s + 2 of B, loaded
   // in slice 3, and step s + 3 of A, loaded in the slices after that, which have more than a step to arrive.  The
   // address unit takes 16 cycles for a load, and a wavefront that finds it busy issues nothing: one load every kGap
-  // matrix instructions.  A checkpoint's codes arrive in registers by the same barrier as the tile of B before them,
-  // and go into the LDS a quarter a slice.
+  // matrix instructions.  A checkpoint's codes are loaded a step before their first use and go into the LDS a quarter a
+  // slice.  (They are waited for earlier than that: the compiler widens the loaded scale bytes at the end of the loop of
+  // two steps, so that every second step waits there for loads that it has just issued, and its waits for codes do not
+  // count the loads written as asm, so that they reach A's tiles too.)
   using SA = Stream<AKC, BM, NW>;
   using SB = Stream<BKC, BN, NW>;
   typename SK::Codes codes[2];
@@ -1239,7 +1242,8 @@ __global__ __launch_bounds__(256, 2) void k_linear_any(int32_t M, int32_t N, int
 // operand and the tokens as the second, straight from memory to registers, 16 bytes a lane, eight loads of the
 // weights in flight (sixteen: 8.6 us against 8.1, past the caches 10.2); float32 as in k_linear_any.  4096 x 4096
 // weights in bfloat16, one token: 8.1 to 9 us, about 4 TB/s, of which 3 us are the launch and the last loads' latency.
-// The eight partial sums are added in order through the LDS.
+// The eight partial sums are added in order through the LDS.  Up to 32 tokens: with those weights 32 take 13.1 us here and
+// 33 12.7 on tiles (16: 9.6), in float32 27.5 and 34.0.
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewWaves = 8;
 constexpr int kFewTokens = 32;

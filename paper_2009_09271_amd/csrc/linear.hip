@@ -117,9 +117,11 @@ constexpr int kCUs = 256;
 // Microseconds that a form takes, fitted to what was measured: for each round of the workgroups that the CUs hold at
 // one time, `few` to `full` for one step along k (from where half of them are at work, one a CU, to all of them:
 // workgroups share a CU, and the chip its power) and `fixed` for the start and the epilogue; then the partial sums
-// written, and the join: a launch, and the sums read.  For instance forward, n, i, o = 2048, 4096, 4096: 128 x 128 tiles
-// 67 measured, 67 by this; 256 x 256 tiles 84 and 82, in two parts of k 79 and 90.  8192, 4096, 4096: 256 x 256 tiles 238
-// and 236.  wgrad of 8192 tokens, 768 x 768, 128 x 128 tiles, in 4, 7 and 14 parts: 34, 28 and 29; 41, 29 and 29.
+// written, and the join: a launch, and the sums read.  For instance forward of normal values, n, i, o = 2048, 4096, 4096:
+// 128 x 128 tiles 63 measured, 67 by this; 256 x 256 tiles 73 and 80, in two parts of k 76 and 93.  8192, 4096, 4096:
+// 256 x 256 tiles 207 and 238 (values of activations: 236).  wgrad of 8192 tokens, 768 x 768, 128 x 128 tiles, in 4, 7, 8
+// and 13 parts: 34, 27, 31 and 27 measured, 42, 33, 32 and 33 by this: the forms are told apart, the parts of k only
+// nearly (8 are taken).
 struct Cost {
   int tile, k, per_cu;
   double few, full, fixed;

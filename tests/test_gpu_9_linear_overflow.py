@@ -100,3 +100,48 @@ def test_an_overflow_reaches_its_columns_of_dw(kernel, dtype, n, i, o, pad, fmt)
         dw, db = run(kernel, dy, q, s, fmt, pad, add)
         assert bool(dw[:, bad].isnan().all()), (int(dw[:, bad].isnan().sum()), dw[:, bad].numel())
         assert torch.equal(dw[:, ~bad].double(), want[:, ~bad] + (add or 0)) and torch.equal(db.double(), dy.double().sum(0) + (add or 0))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("kernel,dtype,n,i,o,pad", [("k_linear_bf16<128> dgrad", "bf16", 200, 512, 256, 0), ("k_linear_bf16<256> dgrad", "bf16", 4096, 4096, 256, 0),
+                                                    ("k_linear_join dgrad", "bf16", 64, 256, 8192, 0), ("k_linear_any dgrad", "bf16", 200, 512, 256, 1),
+                                                    ("k_linear_any dgrad", "f32", 200, 512, 256, 0)])
+def test_an_overflow_reaches_its_group_of_dx(kernel, dtype, n, i, o, pad, fmt):
+    """A group of the kept input of an activation that held an infinity or a NaN makes its 32 values of dx NaN, also
+    where dy is zero, and no others; without an activation nothing of it is read."""
+    import torch
+    announce("overflow dgrad", kernel, dtype, fmt)
+    e, t = E(), {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    z = torch.randint(-3, 4, (n, i), generator=g, device="cuda").float()
+    bad = torch.zeros(n, i, dtype=torch.bool, device="cuda")
+    for row, col, v in ((3, 5, float("inf")), (n - 1, i - 1, float("nan")), (33, 64, float("-inf")), (33, 31, float("inf"))):
+        z[row, col] = v
+        bad[row, col // 32 * 32:col // 32 * 32 + 32] = True
+    q, s = e.ckpt_buffers(n, i)
+    e.ef_ckpt_pack(z, q, s, fmt)
+    dy = torch.randint(-2, 3, (n, o), generator=g, device="cuda").to(t)
+    dy[33] = 0
+    w = torch.randint(-2, 3, (o, i), generator=g, device="cuda").to(t)
+    wide = torch.zeros(n, o + pad, dtype=t, device="cuda")
+    wide[:, :o] = dy
+    p = torch.matmul(dy.double(), w.double())
+    ws = e.linear_workspace(e.EF_OP_DGRAD, n, i, o, t)
+    for act in range(5):
+        dx = torch.empty(n, i, dtype=t, device="cuda")
+        e.timing_enable(True)
+        try:
+            e.ef_linear_dgrad(wide[:, :o], w, dx, ws, act=act, codes=q, scales=s, fmt=fmt)
+            ran = e.timing_collect()
+        finally:
+            e.timing_enable(False)
+        assert kernel in ran, ran
+        dz = torch.empty(n, i, dtype=t, device="cuda")
+        e.ef_ckpt_act_backward(act, q, s, fmt, torch.ones_like(dz), dz)
+        if act == e.EF_ACT_NONE:
+            assert torch.equal(dx.double(), p.to(t).double())
+            continue
+        assert torch.equal(dx.isnan(), bad) and torch.equal(dz.isnan(), bad)
+        if act == e.EF_ACT_RELU:
+            assert torch.equal(dx[~bad].double(), (p * (z > 0)).to(t).double()[~bad])
